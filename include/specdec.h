@@ -41,7 +41,7 @@ extern "C" {
 
 typedef struct specdec_ctx specdec_ctx;
 
-typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1 } specdec_dtype;
+typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1, SPECDEC_F16 = 2 /* the row operators at the end alone */ } specdec_dtype;
 
 typedef enum {
     SPECDEC_OK = 0,
@@ -56,6 +56,8 @@ typedef enum {
 #define SPECDEC_DATA_BAD_TOKEN  2u /* some cand_tokens[b,i] outside [0,V)                */
 #define SPECDEC_DATA_WAIT_LIMIT 4u /* a bounded in-kernel wait gave up (outputs invalid) */
 #define SPECDEC_DATA_TOPK_TIES  8u /* top-k: thousands of logits tie with a row's k-th largest    */
+
+#define SPECDEC_DATA_BAD_PARENT 16u /* specdec_beam_reorder: a parent >= W                         */
 
 /* Kernel selection for specdec_verify_correct (flags argument). 0 lets the library pick. */
 #define SPECDEC_VERIFY_AUTO    0u
@@ -381,6 +383,122 @@ int specdec_verify_correct_static(const void* target_logits, const void* draft_l
                                   int B, int K, int V,
                                   int32_t* n_accepted, int32_t* next_token,
                                   uint32_t* data_status, void* stream, char* err, size_t err_len);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Row operators: what trains a draft model on the target's logits, and a draft that follows several continuations.
+ * (No counterpart in the paper, whose draft model is given and drafts one continuation.)
+ *
+ * They take rows of V logits, f32, bf16 or f16, whose elements follow one another; rows may lie at any stride >= V
+ * and any alignment of whole elements.  Nothing outside a row's V elements is read or written.  Sizes do not depend on
+ * max_B and max_K of the context, which owns no buffer of these calls: calls on several streams may overlap.
+ * V <= 2^22; temperature T in [2^-20, 2^20].  The same call on rows of the same alignment gives the same
+ * bits every time.
+ */
+
+/*
+ * The k largest logits of each row, and its log-sum-exp.
+ *   values  dev out [rows, top_k] f32    descending; equal logits in the order of their tokens; NaN ranks below -inf
+ *   tokens  dev out [rows, top_k] int32  their tokens
+ *   lse     dev out [rows] f32 or NULL   log sum_v exp(logit_v / T): -inf for a row without a logit above -inf,
+ *                                        NaN for a row with NaN or +inf
+ * 1 <= top_k <= min(V, SPECDEC_TOP_LOGITS_MAX).  Terms are summed in fp32 within a thread, in 64 bits beyond it.
+ * Errors: EINVAL (null pointer, extents, stride < V, temperature, dtype, top_k), EUNSUPPORTED (V > 2^22), ECUDA.
+ */
+#define SPECDEC_TOP_LOGITS_MAX 256
+int specdec_top_logits(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int64_t row_stride, int rows, int V,
+                       int top_k, float temperature, float* values, int32_t* tokens, float* lse, void* stream);
+
+/*
+ * Distillation of a draft model from the target's top logits: cross-entropy of the draft's distribution against the
+ * target's on the listed tokens, less the target's entropy (their Kullback-Leibler divergence).  For a row with listed
+ * tokens y_j, target logits v_j and draft logits z, q = softmax(z / T):
+ *   lse given   p_j = exp(v_j/T - lse), R = max(0, 1 - sum_j p_j), Q = sum of q outside the list: all tokens that
+ *               the list leaves out count as one outcome.  A draft with no mass outside the list has no such outcome.
+ *   lse NULL    p_j = exp(v_j/T) / sum_i exp(v_i/T), R = 0: the list is the whole target.
+ *   loss = sum_j p_j (log p_j - log q_{y_j}) + R (log R - log Q)
+ * A token -1 marks an entry that is not there; a row without an entry is padding: loss 0, gradient 0.  A token listed
+ * twice, or outside [-1, V), makes the row's loss NaN and its gradient 0 and sets SPECDEC_DATA_BAD_TOKEN.  A draft row
+ * without a logit above -inf has loss +inf (0 if every p_j is 0) and gradient 0; NaN and +inf in a draft row give NaN.
+ * A listed logit v_j = -inf has p_j = 0.
+ */
+#define SPECDEC_DISTILL_MAX_LIST 1024
+#define SPECDEC_DISTILL_SAVED 4
+typedef struct specdec_distill_rows {
+    const void* logits;         /* dev [rows, V] z, the draft's logits       */
+    specdec_dtype dtype;
+    int64_t row_stride;         /* elements from row to row, >= V            */
+    const float* values;        /* dev [rows, top_k] v                       */
+    const int32_t* tokens;      /* dev [rows, top_k] y                       */
+    const float* lse;           /* dev [rows] or NULL                        */
+    int rows, V, top_k;         /* 1 <= top_k <= SPECDEC_DISTILL_MAX_LIST    */
+    float temperature;          /* T; of the target's lse as well            */
+} specdec_distill_rows;
+
+/* loss dev out [rows] f32; saved dev out [rows, SPECDEC_DISTILL_SAVED] f32: what specdec_distill_backward needs. */
+int specdec_distill(specdec_ctx* ctx, const specdec_distill_rows* rows, float* loss, float* saved, void* stream);
+
+/*
+ * grad[n, :] = row_grad[n] * d loss_n / d z_n, of the logits' type and rounded once.
+ *   saved     dev [rows, SPECDEC_DISTILL_SAVED]  of specdec_distill on the same rows
+ *   row_grad  dev [rows] f32                     gradient of the result in each row's loss; 0: the row's gradient is 0
+ *                                                whatever its logits are, and they are not read
+ *   grad      dev out [rows, V] at grad_stride >= V; it may lie on the logits (same address and stride), which are
+ *             then gone; any other overlap is EINVAL
+ */
+int specdec_distill_backward(specdec_ctx* ctx, const specdec_distill_rows* rows, const float* saved, const float* row_grad,
+                             void* grad, int64_t grad_stride, void* stream);
+
+/* Loss and gradient in one pass over the logits, for a caller that knows the row gradients beforehand (1 / number of
+ * tokens, say): as specdec_distill and specdec_distill_backward with row_grad = row_weight; a row of weight 0 has
+ * loss 0 as well.  The loss itself is not weighted. */
+int specdec_distill_step(specdec_ctx* ctx, const specdec_distill_rows* rows, const float* row_weight, float* loss,
+                         void* grad, int64_t grad_stride, void* stream);
+
+/*
+ * Beam selection: for each of B batch entries the n_out best continuations of its W beams.
+ *   candidate (w, v) has the score  scores[b,w] + logits[b,w,v]/T - log sum_u exp(logits[b,w,u]/T)
+ *   logits      dev [B, W, V]  at batch_stride and beam_stride (elements)
+ *   scores      dev [B, W] f32 sum of log-probabilities so far
+ *   finished    dev [B, W] int32 or NULL: a beam with a value other than 0 offers the one candidate end_token, with the
+ *               score that it has; its logits are not read
+ *   out_scores  dev out [B, n_out] f32    descending; equal scores in the order of (beam, token)
+ *   out_parents dev out [B, n_out] int32  beam that is continued
+ *   out_tokens  dev out [B, n_out] int32  token that continues it
+ * A beam whose score is not finite (an empty place), or whose row has no finite log-sum-exp (all -inf, NaN, +inf),
+ * offers its tokens with the score -inf.  Where there are fewer candidates than n_out the last places hold -inf, -1, -1.
+ * Candidates are ranked in 64 bits; out_scores is rounded once.
+ *   workspace   dev, 16-byte aligned, at least specdec_beam_workspace(B, W, V, n_out) bytes; its contents do not
+ *               matter before the call or after it.  Calls that overlap on the GPU need a workspace each.
+ * 1 <= n_out <= min(W*V, SPECDEC_TOP_LOGITS_MAX); W * min(n_out, V) <= SPECDEC_BEAM_MAX_CANDIDATES.
+ */
+#define SPECDEC_BEAM_MAX_CANDIDATES 8192
+size_t specdec_beam_workspace(int B, int W, int V, int n_out);
+int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int64_t batch_stride, int64_t beam_stride,
+                        const float* scores, const int32_t* finished, int end_token, float temperature,
+                        int B, int W, int V, int n_out, float* out_scores, int32_t* out_parents, int32_t* out_tokens,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Reordering of the beams' states after a selection: beam m of entry b gets the state of beam parents[b, m], for
+ * `outer` layers (or any outer extent) of one buffer.  A beam's state is `runs` stretches of `steps` steps of
+ * step_bytes bytes, the steps of a stretch one after another; of a stretch the first lens[b] steps are moved (all of
+ * them where lens is NULL; lens outside [0, steps] counts as the nearer end), the others stay as they are in dst.
+ *   parents  dev [B, W] int32 at parent_stride (elements) from entry to entry.  A negative parent leaves the beam
+ *            as it is (in dst: a copy of itself); so does one >= W, which sets SPECDEC_DATA_BAD_PARENT.
+ *   src, dst dev, the same strides in both; src == dst reorders in place, without any buffer.  A partial overlap, or
+ *            strides that let two beams share a byte, are EINVAL.
+ * W <= SPECDEC_BEAM_MAX_REORDER.
+ */
+#define SPECDEC_BEAM_MAX_REORDER 128
+typedef struct specdec_beam_state {
+    const void* src;
+    void* dst;
+    int outer, runs, steps;
+    int64_t step_bytes;
+    int64_t outer_stride, batch_stride, beam_stride, run_stride;   /* bytes; ignored where the extent is 1 */
+} specdec_beam_state;
+int specdec_beam_reorder(specdec_ctx* ctx, const int32_t* parents, int64_t parent_stride, const int32_t* lens, int B, int W,
+                         const specdec_beam_state* state, void* stream);
 
 #ifdef __cplusplus
 }

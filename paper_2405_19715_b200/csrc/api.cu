@@ -5,6 +5,7 @@
 #include <cstring>
 #include <new>
 
+#include "row_ops.h"
 #include "specdec_internal.h"
 
 namespace {
@@ -181,7 +182,7 @@ int specdec_device_status(specdec_ctx* ctx, void* stream, uint32_t* bits) {
     CU(ctx, cudaMemsetAsync(ctx->status, 0, sizeof(uint32_t), s));
     CU(ctx, cudaStreamSynchronize(s));
     if (bits) *bits = host;
-    if (host) return fail(ctx, SPECDEC_EDATA, "device status bits 0x%x (1 = bad cand_len, 2 = bad token, 4 = wait limit, 8 = top-k ties)", host);
+    if (host) return fail(ctx, SPECDEC_EDATA, "device status bits 0x%x (1 = bad cand_len, 2 = bad token, 4 = wait limit, 8 = top-k ties, 16 = bad parent)", host);
     return SPECDEC_OK;
 }
 
@@ -529,6 +530,232 @@ int specdec_stop_step(specdec_ctx* ctx, const float* accept_prob_step, float* p_
     if (int rc = specdec_use_device(ctx)) return rc;
     cudaError_t e = launch_stop_step(accept_prob_step, p_hat, h, B, stop, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(ctx, e, "stop_step launch");
+    ctx->launches += 1;
+    return SPECDEC_OK;
+}
+
+namespace {
+constexpr int ROWS_MAX = 1 << 27;                  // rows * cluster size stays within a grid
+
+int check_row_args(specdec_ctx* ctx, const char* who, const void* logits, int dtype, int64_t stride, int rows, int V, float T) {
+    if (dtype != SPECDEC_F32 && dtype != SPECDEC_BF16 && dtype != SPECDEC_F16) return fail(ctx, SPECDEC_EINVAL, "%s: unknown dtype %d", who, dtype);
+    if (rows < 1 || V < 1) return fail(ctx, SPECDEC_EINVAL, "%s: the number of rows and V must be >= 1 (got %d, %d)", who, rows, V);
+    if (V > (1 << 22)) return fail(ctx, SPECDEC_EUNSUPPORTED, "%s: V=%d above 2^22", who, V);
+    if (rows > ROWS_MAX) return fail(ctx, SPECDEC_EUNSUPPORTED, "%s: %d rows, above 2^27", who, rows);
+    if (stride < V) return fail(ctx, SPECDEC_EINVAL, "%s: a row stride of %lld elements, below V=%d", who, (long long)stride, V);
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == SPECDEC_F32 ? 4 : 2) != 0)
+        return fail(ctx, SPECDEC_EINVAL, "%s: logits must be aligned to their element", who);
+    // 2^-20 to 2^20: log2(e)/T and its product with any difference of logits that matters stay ordinary numbers
+    if (!(T >= 9.5367431640625e-7f && T <= 1048576.f)) return fail(ctx, SPECDEC_EINVAL, "%s: temperature must be in [2^-20, 2^20]", who);
+    return SPECDEC_OK;
+}
+rw::Scale make_scale(double T) {
+    const double c = 1.4426950408889634074 / T;
+    float hi = (float)c;
+    if ((double)hi > c) hi = std::nextafterf(hi, 0.f);
+    const float lo = (float)(c - (double)hi);
+    return rw::Scale{hi, lo > 1e-37f ? lo : 1e-37f};
+}
+
+int distill(specdec_ctx* ctx, const char* who, DistillMode mode, const specdec_distill_rows* r, float* loss, float* saved, const float* weight,
+            void* grad, int64_t grad_stride, cudaStream_t s) {
+    if (!r || !r->logits || !r->values || !r->tokens) return fail(ctx, SPECDEC_EINVAL, "%s: null pointer argument", who);
+    if ((mode != DistillMode::Gradient && !loss) || (mode != DistillMode::Step && !saved) || (mode != DistillMode::Loss && (!weight || !grad)))
+        return fail(ctx, SPECDEC_EINVAL, "%s: null pointer argument", who);
+    if (int rc = check_row_args(ctx, who, r->logits, (int)r->dtype, r->row_stride, r->rows, r->V, r->temperature)) return rc;
+    if (r->top_k < 1 || r->top_k > SPECDEC_DISTILL_MAX_LIST) return fail(ctx, SPECDEC_EINVAL, "%s: top_k must be in [1, %d] (got %d)", who, SPECDEC_DISTILL_MAX_LIST, r->top_k);
+    if (mode != DistillMode::Loss) {
+        const int64_t es = r->dtype == SPECDEC_F32 ? 4 : 2;
+        if (grad_stride < r->V) return fail(ctx, SPECDEC_EINVAL, "%s: a gradient row stride of %lld elements, below V=%d", who, (long long)grad_stride, r->V);
+        if (reinterpret_cast<uintptr_t>(grad) % es != 0) return fail(ctx, SPECDEC_EINVAL, "%s: the gradient must be aligned to its element", who);
+        // the gradient may lie on the logits, row on row; any other overlap would overwrite logits that are still to be read
+        const uintptr_t z = reinterpret_cast<uintptr_t>(r->logits), g = reinterpret_cast<uintptr_t>(grad);
+        const uintptr_t z_end = z + ((uintptr_t)(r->rows - 1) * r->row_stride + r->V) * es, g_end = g + ((uintptr_t)(r->rows - 1) * grad_stride + r->V) * es;
+        if (z < g_end && g < z_end && !(z == g && (r->row_stride == grad_stride || r->rows == 1)))
+            return fail(ctx, SPECDEC_EINVAL, "%s: the gradient overlaps the logits without lying on them", who);
+    }
+    DistillParams p = {};
+    p.z = r->logits;
+    p.z_stride = r->row_stride;
+    p.values = r->values;
+    p.tokens = r->tokens;
+    p.lse = r->lse;
+    p.V = r->V;
+    p.k = r->top_k;
+    p.T = (double)r->temperature;
+    p.log2e_t = 1.4426950408889634074 / p.T;
+    p.c = make_scale(p.T);
+    p.loss = loss;
+    p.saved = saved;
+    p.weight = weight;
+    p.grad = grad;
+    p.g_stride = grad_stride;
+    p.status = ctx->status;
+    cudaError_t e = launch_distill(p, r->dtype, mode, r->rows, ctx->sm_count, s);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, who);
+    ctx->launches += 1;
+    return SPECDEC_OK;
+}
+}  // namespace
+
+int specdec_top_logits(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int64_t row_stride, int rows, int V, int top_k, float temperature,
+                       float* values, int32_t* tokens, float* lse, void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (!logits || !values || !tokens) return fail(ctx, SPECDEC_EINVAL, "top_logits: null pointer argument");
+    if (int rc = check_row_args(ctx, "top_logits", logits, (int)dtype, row_stride, rows, V, temperature)) return rc;
+    if (top_k < 1 || top_k > SPECDEC_TOP_LOGITS_MAX || top_k > V)
+        return fail(ctx, SPECDEC_EINVAL, "top_logits: top_k must be in [1, min(V, %d)] (got %d)", SPECDEC_TOP_LOGITS_MAX, top_k);
+    if (int rc = specdec_use_device(ctx)) return rc;
+    TopParams p = {};
+    p.x = logits;
+    p.row_stride = row_stride;
+    p.inner = rows;
+    p.V = V;
+    p.k = top_k;
+    p.T = (double)temperature;
+    p.log2e_t = 1.4426950408889634074 / p.T;
+    p.c = make_scale(p.T);
+    p.values = values;
+    p.tokens = tokens;
+    p.lse = lse;
+    cudaError_t e = launch_top_logits(p, dtype, rows, ctx->sm_count, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "top_logits launch");
+    ctx->launches += 1;
+    return SPECDEC_OK;
+}
+
+int specdec_distill(specdec_ctx* ctx, const specdec_distill_rows* rows, float* loss, float* saved, void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (int rc = specdec_use_device(ctx)) return rc;
+    return distill(ctx, "distill", DistillMode::Loss, rows, loss, saved, nullptr, nullptr, 0, static_cast<cudaStream_t>(stream));
+}
+
+int specdec_distill_backward(specdec_ctx* ctx, const specdec_distill_rows* rows, const float* saved, const float* row_grad, void* grad,
+                             int64_t grad_stride, void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (int rc = specdec_use_device(ctx)) return rc;
+    return distill(ctx, "distill_backward", DistillMode::Gradient, rows, nullptr, const_cast<float*>(saved), row_grad, grad, grad_stride,
+                   static_cast<cudaStream_t>(stream));
+}
+
+int specdec_distill_step(specdec_ctx* ctx, const specdec_distill_rows* rows, const float* row_weight, float* loss, void* grad, int64_t grad_stride,
+                         void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (int rc = specdec_use_device(ctx)) return rc;
+    return distill(ctx, "distill_step", DistillMode::Step, rows, loss, nullptr, row_weight, grad, grad_stride, static_cast<cudaStream_t>(stream));
+}
+
+size_t specdec_beam_workspace(int B, int W, int V, int n_out) {
+    if (B < 1 || W < 1 || V < 1 || n_out < 1) return 0;
+    const size_t rows = (size_t)B * W, k = n_out < V ? n_out : V;
+    return align_up(rows * sizeof(rw::Part), 256) + 2 * align_up(rows * k * 4, 256);
+}
+
+int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int64_t batch_stride, int64_t beam_stride, const float* scores,
+                        const int32_t* finished, int end_token, float temperature, int B, int W, int V, int n_out, float* out_scores,
+                        int32_t* out_parents, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (!logits || !scores || !out_scores || !out_parents || !out_tokens || !workspace) return fail(ctx, SPECDEC_EINVAL, "beam_select: null pointer argument");
+    if (B < 1 || W < 1) return fail(ctx, SPECDEC_EINVAL, "beam_select: B and W must be >= 1 (got %d, %d)", B, W);
+    if ((long long)B * W > ROWS_MAX) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_select: %lld beams, above 2^27", (long long)B * W);
+    if (int rc = check_row_args(ctx, "beam_select", logits, (int)dtype, beam_stride, B * W, V, temperature)) return rc;
+    if (batch_stride < 0 || (B > 1 && batch_stride < V)) return fail(ctx, SPECDEC_EINVAL, "beam_select: a batch stride of %lld elements", (long long)batch_stride);
+    if (finished && (end_token < 0 || end_token >= V)) return fail(ctx, SPECDEC_EINVAL, "beam_select: end_token %d outside [0, %d)", end_token, V);
+    if (n_out < 1 || n_out > SPECDEC_TOP_LOGITS_MAX || (long long)n_out > (long long)W * V)
+        return fail(ctx, SPECDEC_EINVAL, "beam_select: n_out must be in [1, min(W*V, %d)] (got %d)", SPECDEC_TOP_LOGITS_MAX, n_out);
+    const int k = n_out < V ? n_out : V;
+    if ((long long)W * k > SPECDEC_BEAM_MAX_CANDIDATES)
+        return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_select: %d beams with %d candidates each, above %d in all", W, k, SPECDEC_BEAM_MAX_CANDIDATES);
+    if ((long long)W * V > 0x7fffffffll) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_select: W*V above 2^31");
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return fail(ctx, SPECDEC_EINVAL, "beam_select: the workspace must be 16-byte aligned");
+    if (workspace_bytes < specdec_beam_workspace(B, W, V, n_out))
+        return fail(ctx, SPECDEC_EINVAL, "beam_select: a workspace of %zu bytes, %zu needed", workspace_bytes, specdec_beam_workspace(B, W, V, n_out));
+    if (int rc = specdec_use_device(ctx)) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const size_t rows = (size_t)B * W;
+    char* ws = static_cast<char*>(workspace);
+    TopParams t = {};
+    t.x = logits;
+    t.outer_stride = batch_stride;
+    t.row_stride = beam_stride;
+    t.inner = W;
+    t.V = V;
+    t.k = k;
+    t.T = (double)temperature;
+    t.log2e_t = 1.4426950408889634074 / t.T;
+    t.c = make_scale(t.T);
+    t.parts = reinterpret_cast<rw::Part*>(ws);
+    t.values = reinterpret_cast<float*>(ws + align_up(rows * sizeof(rw::Part), 256));
+    t.tokens = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(t.values) + align_up(rows * k * 4, 256));
+    t.scores = scores;
+    t.finished = finished;
+    cudaError_t e = launch_top_logits(t, dtype, (int)rows, ctx->sm_count, s);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "beam_select launch");
+    BeamParams p = {};
+    p.values = t.values;
+    p.tokens = t.tokens;
+    p.parts = t.parts;
+    p.scores = scores;
+    p.finished = finished;
+    p.W = W;
+    p.V = V;
+    p.k = k;
+    p.M = n_out;
+    p.end_token = end_token;
+    p.c = t.c;
+    p.T = t.T;
+    p.out_scores = out_scores;
+    p.out_parents = out_parents;
+    p.out_tokens = out_tokens;
+    e = launch_beam_merge(p, B, s);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "beam_select launch");
+    ctx->launches += 2;
+    return SPECDEC_OK;
+}
+
+int specdec_beam_reorder(specdec_ctx* ctx, const int32_t* parents, int64_t parent_stride, const int32_t* lens, int B, int W,
+                         const specdec_beam_state* state, void* stream) {
+    if (!ctx) return SPECDEC_EINVAL;
+    if (!parents || !state || !state->src || !state->dst) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: null pointer argument");
+    if (B < 1 || W < 1 || state->outer < 1 || state->runs < 1 || state->steps < 1 || state->step_bytes < 1)
+        return fail(ctx, SPECDEC_EINVAL, "beam_reorder: every extent must be >= 1");
+    if (W > SPECDEC_BEAM_MAX_REORDER) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_reorder: %d beams, above %d", W, SPECDEC_BEAM_MAX_REORDER);
+    if (parent_stride < W) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: a parent stride of %lld, below W=%d", (long long)parent_stride, W);
+    // no two beams may share a byte: dimension by dimension from the smallest stride, each steps over all below it
+    struct Dim { int64_t n, stride; } d[4] = {{state->outer, state->outer_stride}, {B, state->batch_stride}, {W, state->beam_stride}, {state->runs, state->run_stride}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j)
+            if (d[j].stride < d[i].stride) { const Dim t = d[i]; d[i] = d[j]; d[j] = t; }
+    if (state->step_bytes > (1ll << 40) / state->steps) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_reorder: a run above 2^40 bytes");
+    int64_t span = (int64_t)state->steps * state->step_bytes;
+    for (const Dim& x : d) {
+        if (x.n == 1) continue;
+        if (x.stride < span || x.stride > (1ll << 46) / x.n) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: a stride of %lld bytes lets beams overlap, or is too large", (long long)x.stride);
+        span += (x.n - 1) * x.stride;
+    }
+    const uintptr_t a = reinterpret_cast<uintptr_t>(state->src), b = reinterpret_cast<uintptr_t>(state->dst);
+    if (a != b && a < b + span && b < a + span) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: src and dst overlap without being the same");
+    if (int rc = specdec_use_device(ctx)) return rc;
+    ReorderParams p = {};
+    p.src = static_cast<const char*>(state->src);
+    p.dst = static_cast<char*>(state->dst);
+    p.outer_stride = state->outer > 1 ? state->outer_stride : 0;      // a stride that is never taken says nothing about alignment
+    p.batch_stride = B > 1 ? state->batch_stride : 0;
+    p.beam_stride = W > 1 ? state->beam_stride : 0;
+    p.run_stride = state->runs > 1 ? state->run_stride : 0;
+    p.step_bytes = state->step_bytes;
+    p.run_bytes = (int64_t)state->steps * state->step_bytes;
+    p.outer = state->outer;
+    p.runs = state->runs;
+    p.B = B;
+    p.W = W;
+    p.parents = parents;
+    p.parent_stride = parent_stride;
+    p.lens = lens;
+    p.status = ctx->status;
+    cudaError_t e = launch_beam_reorder(p, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorInvalidConfiguration) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_reorder: the state is too large for one launch");
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "beam_reorder launch");
     ctx->launches += 1;
     return SPECDEC_OK;
 }

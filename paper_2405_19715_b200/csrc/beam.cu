@@ -1,0 +1,245 @@
+// Beam selection over the vocabulary rows of W beams, and the reordering of the beams' states that follows it.
+//
+// Selection.  Candidate (w, v) of a batch entry has the score s_w + x_{w,v}/T - lse_w.  Within a beam the order is that
+// of the logits, so the best M of all beams are among the best M of each: the row kernel of top_logits.cu makes those
+// lists and the sums behind lse_w in one pass over the logits, and one CTA per batch entry ranks the W*M candidates.
+// They are ranked in 64 bits: beams differ by sums of many terms, and two candidates that fp32 cannot tell apart would
+// come out in an order of chance.
+#include "rows.cuh"
+
+namespace {
+
+using namespace rw;
+
+__device__ __forceinline__ unsigned long long score_key(double s) {
+    const unsigned long long b = (unsigned long long)__double_as_longlong(s + 0.0);
+    return (b >> 63) ? ~b : (b | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double key_score(unsigned long long key) {
+    return __longlong_as_double((long long)((key >> 63) ? (key & 0x7fffffffffffffffull) : ~key));
+}
+__device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
+
+__global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    const int n = P.W * P.k;
+    unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // 0: no candidate
+    int* flat = reinterpret_cast<int*>(keys + n);                               // w * V + v
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int mine = 0;
+    for (int w = warp; w < P.W; w += WARPS) {
+        const int row = b * P.W + w;
+        const float s = P.scores[row];
+        const bool ended = P.finished && P.finished[row], live = s > -INFINITY && s < INFINITY;
+        double lse = 0.0;
+        bool open = live && !ended;
+        if (open) {
+            // lse in 64 bits: the listed terms, the largest of the sum, are exchanged for exact ones
+            const Part part = P.parts[row];
+            const float m = reference(part.m);
+            double fix = 0.0;
+            for (int i = lane; i < P.k; i += 32) {
+                const float x = P.values[(size_t)row * P.k + i];
+                fix += exp(((double)x - (double)m) / P.T) - (double)term(x, m, P.c);
+            }
+            lse = (double)m / P.T + log(part.s + warp_sum(fix));
+            open = is_finite(lse);                  // a row without a finite sum offers nothing
+        }
+        for (int i = lane; i < P.k; i += 32) {
+            const int o = w * P.k + i;
+            unsigned long long key = 0;
+            int v = 0;
+            if (ended) {
+                if (i == 0) key = score_key(live ? (double)s : -INFINITY);
+                v = P.end_token;
+            } else if (open) {
+                v = P.tokens[(size_t)row * P.k + i];
+                key = score_key((double)s + ((double)P.values[(size_t)row * P.k + i] / P.T - lse));
+            } else {                                // every candidate has -inf: the lowest tokens come first
+                v = i;
+                key = score_key(-INFINITY);
+            }
+            keys[o] = key;
+            flat[o] = w * P.V + v;
+            mine += key != 0;
+        }
+    }
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    __shared__ int counts[WARPS];
+    if (lane == 0) counts[warp] = mine;
+    __syncthreads();
+    for (int i = tid; i < n; i += THREADS) {
+        const unsigned long long key = keys[i];
+        if (key == 0) continue;
+        const int f = flat[i];
+        int place = 0;
+        for (int q = 0; q < n; ++q) place += keys[q] > key || (keys[q] == key && flat[q] < f);
+        if (place < P.M) {
+            const size_t o = (size_t)b * P.M + place;
+            P.out_scores[o] = (float)key_score(key);
+            P.out_parents[o] = f / P.V;
+            P.out_tokens[o] = f % P.V;
+        }
+    }
+    int total = 0;
+    for (int w = 0; w < WARPS; ++w) total += counts[w];
+    for (int i = total + tid; i < P.M; i += THREADS) {          // fewer candidates than places
+        const size_t o = (size_t)b * P.M + i;
+        P.out_scores[o] = -INFINITY;
+        P.out_parents[o] = -1;
+        P.out_tokens[o] = -1;
+    }
+}
+
+// Reordering.  A thread owns a column: the same few bytes of all W beams of one batch entry.  It loads the column of
+// every beam that changes before it stores any, so states can be reordered in place without a copy or a barrier:
+// nobody else touches its column.  Beams that are their own parent are neither read nor written.
+constexpr int COPY_THREADS = 256;
+
+template <typename U, int WMAX, int COLS>
+__global__ void __launch_bounds__(COPY_THREADS) beam_reorder_kernel(const __grid_constant__ ReorderParams P, long long chunks) {
+    long long task = blockIdx.x;
+    const long long chunk = task % chunks;
+    task /= chunks;
+    const int run = (int)(task % P.runs);
+    task /= P.runs;
+    const int b = (int)(task % P.B);
+    const int o = (int)(task / P.B);
+    long long bytes = P.run_bytes;
+    if (P.lens) bytes = min(bytes, (long long)max(P.lens[b], 0) * P.step_bytes);
+    const bool in_place = P.src == P.dst;
+    const int32_t* parents = P.parents + b * P.parent_stride;
+    if (chunk == 0 && run == 0 && o == 0 && threadIdx.x < P.W && parents[threadIdx.x] >= P.W)
+        atomicOr(P.status, SPECDEC_DATA_BAD_PARENT);
+    const long long at0 = chunk * (long long)(COPY_THREADS * COLS * sizeof(U));
+    if (at0 >= bytes) return;
+    const long long first = o * P.outer_stride + b * P.batch_stride + run * P.run_stride;
+    const char* src = P.src + first;
+    char* dst = P.dst + first;
+    int from[WMAX];
+#pragma unroll
+    for (int m = 0; m < WMAX; ++m) {
+        const int p = m < P.W ? parents[m] : m;
+        from[m] = m >= P.W ? -1 : p >= 0 && p < P.W ? (in_place && p == m ? -1 : p) : (in_place ? -1 : m);
+    }
+    U v[COLS][WMAX];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) {
+        const long long at = at0 + ((long long)c * COPY_THREADS + threadIdx.x) * sizeof(U);
+#pragma unroll
+        for (int m = 0; m < WMAX; ++m)
+            if (from[m] >= 0 && at + (long long)sizeof(U) <= bytes) v[c][m] = *reinterpret_cast<const U*>(src + from[m] * P.beam_stride + at);
+    }
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) {
+        const long long at = at0 + ((long long)c * COPY_THREADS + threadIdx.x) * sizeof(U);
+#pragma unroll
+        for (int m = 0; m < WMAX; ++m)
+            if (from[m] >= 0 && at + (long long)sizeof(U) <= bytes) *reinterpret_cast<U*>(dst + m * P.beam_stride + at) = v[c][m];
+    }
+    // the last bytes of a run that is no multiple of the column
+    if constexpr (sizeof(U) > 1) {
+        const long long tail = bytes - bytes % (long long)sizeof(U), at = tail + threadIdx.x;
+        if (tail >= at0 && tail < at0 + (long long)(COPY_THREADS * COLS * sizeof(U)) && at < bytes) {
+            char w[WMAX];
+#pragma unroll
+            for (int m = 0; m < WMAX; ++m)
+                if (from[m] >= 0) w[m] = src[from[m] * P.beam_stride + at];
+#pragma unroll
+            for (int m = 0; m < WMAX; ++m)
+                if (from[m] >= 0) dst[m * P.beam_stride + at] = w[m];
+        }
+    }
+}
+
+// More beams than a thread's registers hold: the column waits in shared memory, still the thread's own.
+template <typename U>
+__global__ void __launch_bounds__(64) beam_reorder_wide_kernel(const __grid_constant__ ReorderParams P, long long chunks) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    U* col = reinterpret_cast<U*>(raw) + threadIdx.x;              // entry m of this thread's column: col[m * 64]
+    long long task = blockIdx.x;
+    const long long chunk = task % chunks;
+    task /= chunks;
+    const int run = (int)(task % P.runs);
+    task /= P.runs;
+    const int b = (int)(task % P.B);
+    const int o = (int)(task / P.B);
+    long long bytes = P.run_bytes;
+    if (P.lens) bytes = min(bytes, (long long)max(P.lens[b], 0) * P.step_bytes);
+    const bool in_place = P.src == P.dst;
+    const int32_t* parents = P.parents + b * P.parent_stride;
+    if (chunk == 0 && run == 0 && o == 0)
+        for (int m = threadIdx.x; m < P.W; m += 64)
+            if (parents[m] >= P.W) atomicOr(P.status, SPECDEC_DATA_BAD_PARENT);
+    const long long at0 = chunk * (long long)(64 * sizeof(U)), at = at0 + threadIdx.x * (long long)sizeof(U);
+    if (at0 >= bytes) return;
+    const long long first = o * P.outer_stride + b * P.batch_stride + run * P.run_stride;
+    const char* src = P.src + first;
+    char* dst = P.dst + first;
+    auto from = [&](int m) {
+        const int p = parents[m];
+        return p >= 0 && p < P.W ? (in_place && p == m ? -1 : p) : (in_place ? -1 : m);
+    };
+    if (at + (long long)sizeof(U) <= bytes) {
+        for (int m = 0; m < P.W; ++m)
+            if (const int p = from(m); p >= 0) col[m * 64] = *reinterpret_cast<const U*>(src + p * P.beam_stride + at);
+        for (int m = 0; m < P.W; ++m)
+            if (from(m) >= 0) *reinterpret_cast<U*>(dst + m * P.beam_stride + at) = col[m * 64];
+    }
+    if constexpr (sizeof(U) > 1) {
+        const long long tail = bytes - bytes % (long long)sizeof(U), t = tail + threadIdx.x;
+        if (tail >= at0 && tail < at0 + (long long)(64 * sizeof(U)) && t < bytes) {
+            char* c1 = reinterpret_cast<char*>(col);
+            for (int m = 0; m < P.W; ++m)
+                if (const int p = from(m); p >= 0) c1[m * 64 * sizeof(U)] = src[p * P.beam_stride + t];
+            for (int m = 0; m < P.W; ++m)
+                if (from(m) >= 0) dst[m * P.beam_stride + t] = c1[m * 64 * sizeof(U)];
+        }
+    }
+}
+
+template <typename U>
+cudaError_t reorder_as(const ReorderParams& p, cudaStream_t s) {
+    const long long tasks = (long long)p.outer * p.B * p.runs;
+    if (p.W <= 16) {
+        const int cols = p.W <= 4 ? 4 : p.W <= 8 ? 2 : 1;
+        const long long chunk = (long long)COPY_THREADS * cols * sizeof(U), chunks = (p.run_bytes + chunk - 1) / chunk;
+        if (tasks * chunks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+        const unsigned grid = (unsigned)(tasks * chunks);
+        if (p.W <= 4) beam_reorder_kernel<U, 4, 4><<<grid, COPY_THREADS, 0, s>>>(p, chunks);
+        else if (p.W <= 8) beam_reorder_kernel<U, 8, 2><<<grid, COPY_THREADS, 0, s>>>(p, chunks);
+        else beam_reorder_kernel<U, 16, 1><<<grid, COPY_THREADS, 0, s>>>(p, chunks);
+    } else {
+        const long long chunk = 64ll * sizeof(U), chunks = (p.run_bytes + chunk - 1) / chunk;
+        const size_t smem = (size_t)p.W * chunk;
+        if (tasks * chunks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+        const cudaError_t e = cudaFuncSetAttribute(beam_reorder_wide_kernel<U>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        beam_reorder_wide_kernel<U><<<(unsigned)(tasks * chunks), 64, smem, s>>>(p, chunks);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t beam_merge_smem(int W, int k) { return (size_t)W * k * (sizeof(unsigned long long) + sizeof(int)); }
+
+cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s) {
+    const size_t smem = beam_merge_smem(p.W, p.k);
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    beam_merge_kernel<<<B, rw::THREADS, smem, s>>>(p);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t s) {
+    // the widest column that every address is a multiple of
+    const unsigned long long a = reinterpret_cast<uintptr_t>(p.src) | reinterpret_cast<uintptr_t>(p.dst) | (unsigned long long)p.outer_stride |
+                                 (unsigned long long)p.batch_stride | (unsigned long long)p.beam_stride | (unsigned long long)p.run_stride;
+    if (a % 16 == 0) return reorder_as<uint4>(p, s);
+    if (a % 4 == 0) return reorder_as<uint32_t>(p, s);
+    if (a % 2 == 0) return reorder_as<uint16_t>(p, s);
+    return reorder_as<uint8_t>(p, s);
+}

@@ -1,0 +1,83 @@
+// Launchers of the vocabulary-row operators (top_logits.cu, beam.cu, distill.cu); arguments are checked in api.cu.
+#pragma once
+
+#include "specdec_internal.h"
+
+namespace rw {
+
+// log2(e)/T in two floats: its rounding to one would put the same relative error of 6e-8 * |x - m| into every term of
+// a sum.  hi is rounded down, so that lo is positive and a term of -inf stays 2^-inf.
+struct Scale {
+    float hi, lo;
+};
+
+// Sum of 2^((x - m) * log2(e)/T) over a part of a row, m the part's largest value (-inf: nothing above it, s is then
+// a sum against 0).
+struct Part {
+    double s;
+    float m;
+};
+
+}  // namespace rw
+
+struct TopParams {
+    const void* x;
+    long long outer_stride, row_stride;       // elements; row i is outer i / inner, row i % inner
+    int inner, V, k, cluster;
+    rw::Scale c;
+    double T, log2e_t;
+    float* values;                            // [rows, k]
+    int32_t* tokens;                          // [rows, k]
+    float* lse;                               // [rows] or null
+    rw::Part* parts;                          // [rows] or null: the same before the logarithm
+    const float* scores;                      // [rows] or null: rows whose score is not finite,
+    const int32_t* finished;                  // [rows] or null: or that have finished, are not read
+};
+cudaError_t launch_top_logits(TopParams p, specdec_dtype dtype, int rows, int sm_count, cudaStream_t s);
+
+struct BeamParams {
+    const float* values;                      // [B * W, k] lists of the live beams
+    const int32_t* tokens;
+    const rw::Part* parts;                    // [B * W]
+    const float* scores;                      // [B * W]
+    const int32_t* finished;                  // [B * W] or null
+    int W, V, k, M, end_token;
+    rw::Scale c;
+    double T;
+    float* out_scores;                        // [B, M]
+    int32_t* out_parents;
+    int32_t* out_tokens;
+};
+size_t beam_merge_smem(int W, int k);
+cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s);
+
+struct ReorderParams {
+    const char* src;
+    char* dst;
+    long long outer_stride, batch_stride, beam_stride, run_stride, step_bytes, run_bytes;   // bytes
+    int outer, runs, B, W;
+    const int32_t* parents;
+    long long parent_stride;
+    const int32_t* lens;
+    uint32_t* status;
+};
+cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t s);
+
+struct DistillParams {
+    const void* z;
+    long long z_stride;
+    const float* values;
+    const int32_t* tokens;
+    const float* lse;                         // null: renormalised over the list
+    int V, k, cluster, slice_words;
+    rw::Scale c;
+    double T, log2e_t;
+    float* loss;
+    float* saved;                             // [rows, 4]: written by the loss alone, read by the gradient alone
+    const float* weight;                      // [rows]: gradient of the result in each row's loss
+    void* grad;
+    long long g_stride;
+    uint32_t* status;
+};
+enum class DistillMode { Loss, Gradient, Step };
+cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mode, int rows, int sm_count, cudaStream_t s);

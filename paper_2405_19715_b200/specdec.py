@@ -12,19 +12,24 @@ import torch
 
 from . import build as _build
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 OK, EINVAL, EUNSUPPORTED, ECUDA, EDATA = 0, 1, 2, 3, 4
 VERIFY_AUTO, VERIFY_DIRECT, VERIFY_STREAM, VERIFY_FUSED, VERIFY_CLUSTER = 0, 1, 2, 3, 4
 DATA_BAD_LENGTH, DATA_BAD_TOKEN, DATA_WAIT_LIMIT, DATA_TOPK_TIES = 1, 2, 4, 8
+DATA_BAD_PARENT = 16
 VERIFY_EARLY_EXIT = 0x100
 
 EXPORTS = ["specdec_create", "specdec_destroy", "specdec_last_error", "specdec_device_status",
            "specdec_launch_count", "specdec_last_kernel", "specdec_set_phase_stamps", "specdec_early_exit_count", "specdec_head_launch_mode", "specdec_verify_correct", "specdec_verify_correct_host",
            "specdec_accept_head", "specdec_stop", "specdec_verify_correct_static", "specdec_verify_greedy", "specdec_stop_step", "specdec_selftest_wait_limit", "specdec_verify_correct_topk", "specdec_sample",
-           "specdec_shard_stats", "specdec_shard_accept", "specdec_shard_draw"]
+           "specdec_shard_stats", "specdec_shard_accept", "specdec_shard_draw",
+           "specdec_top_logits", "specdec_distill", "specdec_distill_backward", "specdec_distill_step",
+           "specdec_beam_workspace", "specdec_beam_select", "specdec_beam_reorder"]
 SHARD_STATS_WIDTH, SHARD_MAX_RANKS = 8, 64
 STATIC_MAX_UNITS, STATIC_MAX_V = 16384, 262144
 STAMP_SLOTS = 32
+TOP_LOGITS_MAX, DISTILL_MAX_LIST, DISTILL_SAVED = 256, 1024, 4
+BEAM_MAX_CANDIDATES, BEAM_MAX_REORDER = 8192, 128
 
 
 class SpecdecError(RuntimeError):
@@ -41,6 +46,18 @@ class _Head(C.Structure):
 class _Shard(C.Structure):
     _fields_ = [("target_logits", C.c_void_p), ("draft_logits", C.c_void_p), ("dtype", C.c_int),
                 ("V_shard", C.c_int), ("v_offset", C.c_int), ("V", C.c_int)]
+
+
+class _DistillRows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int), ("row_stride", C.c_int64), ("values", C.c_void_p),
+                ("tokens", C.c_void_p), ("lse", C.c_void_p), ("rows", C.c_int), ("V", C.c_int), ("top_k", C.c_int),
+                ("temperature", C.c_float)]
+
+
+class _BeamState(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("outer", C.c_int), ("runs", C.c_int), ("steps", C.c_int),
+                ("step_bytes", C.c_int64), ("outer_stride", C.c_int64), ("batch_stride", C.c_int64),
+                ("beam_stride", C.c_int64), ("run_stride", C.c_int64)]
 
 
 _lib = None
@@ -88,6 +105,18 @@ def load_library(path: str | Path | None = None) -> C.CDLL:
                                           C.c_void_p]
     lib.specdec_verify_correct_static.argtypes = [vp, vp, C.c_int, ip, ip, fp, C.c_float, C.c_int, C.c_int, C.c_int,
                                                   ip, ip, C.c_void_p, C.c_void_p, C.c_char_p, C.c_size_t]
+    i64 = C.c_int64
+    lib.specdec_top_logits.argtypes = [C.c_void_p, vp, C.c_int, i64, C.c_int, C.c_int, C.c_int, C.c_float, fp, ip, fp,
+                                       C.c_void_p]
+    dp = C.POINTER(_DistillRows)
+    lib.specdec_distill.argtypes = [C.c_void_p, dp, fp, fp, C.c_void_p]
+    lib.specdec_distill_backward.argtypes = [C.c_void_p, dp, fp, fp, vp, i64, C.c_void_p]
+    lib.specdec_distill_step.argtypes = [C.c_void_p, dp, fp, fp, vp, i64, C.c_void_p]
+    lib.specdec_beam_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int]
+    lib.specdec_beam_workspace.restype = C.c_size_t
+    lib.specdec_beam_select.argtypes = [C.c_void_p, vp, C.c_int, i64, i64, fp, ip, C.c_int, C.c_float, C.c_int, C.c_int,
+                                        C.c_int, C.c_int, fp, ip, ip, vp, C.c_size_t, C.c_void_p]
+    lib.specdec_beam_reorder.argtypes = [C.c_void_p, ip, i64, ip, C.c_int, C.c_int, C.POINTER(_BeamState), C.c_void_p]
     if path is None:
         _lib = lib
     return lib
@@ -404,3 +433,225 @@ def specdec_verify_correct_static(target_logits, draft_logits, cand_tokens, cand
     if rc != OK:
         raise SpecdecError(rc, err.value.decode())
     return n_accepted, next_token
+
+
+# ---- row operators ------------------------------------------------------------------------------------------------
+
+_ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _row_dtype(t: torch.Tensor) -> int:
+    if t.dtype not in _ROW_DTYPES:
+        raise ValueError(f"logits must be float32, bfloat16 or float16, got {t.dtype}")
+    return _ROW_DTYPES[t.dtype]
+
+
+def _on(ctx: Context, *tensors):
+    """Every tensor lives on the context's GPU: its pointers mean nothing to another."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != ctx.device):
+            raise ValueError(f"tensor is on {t.device}, the context on cuda:{ctx.device}")
+
+
+def _row_stream(ctx: Context, stream):
+    return stream if stream is not None else torch.cuda.current_stream(ctx.device)
+
+
+def _empty(ctx: Context, stream, shape, dtype):
+    """A tensor of the stream that the call runs on (the allocator hands memory out by stream)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+
+
+def _rows_of(t: torch.Tensor, V: int | None = None):
+    """(pointer, row stride) of a [rows, V] tensor whose rows' elements follow one another."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("expected [rows, V] with adjacent elements in a row")
+    if V is not None and t.shape[1] != V:
+        raise ValueError(f"expected rows of {V}, got {t.shape[1]}")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _shaped(t: torch.Tensor | None, shape, dtype):
+    """Pointer of a contiguous tensor of this shape and type."""
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype)
+
+
+def specdec_top_logits(ctx: Context, logits, top_k: int, temperature: float = 1.0, values=None, tokens=None, lse=None,
+                       stream=None):
+    """specdec_top_logits of the C ABI: logits [rows, V] -> (values [rows, k] f32, tokens [rows, k] int32, lse [rows] f32)."""
+    _on(ctx, logits, values, tokens, lse)
+    ptr, stride = _rows_of(logits)
+    (rows, V), k = logits.shape, int(top_k)
+    if values is None:
+        values = _empty(ctx, stream, (rows, k), torch.float32)
+    if tokens is None:
+        tokens = _empty(ctx, stream, (rows, k), torch.int32)
+    if lse is None:
+        lse = _empty(ctx, stream, (rows,), torch.float32)
+    ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, float(temperature),
+                                          _shaped(values, (rows, k), torch.float32), _shaped(tokens, (rows, k), torch.int32),
+                                          _shaped(lse, (rows,), torch.float32), _row_stream(ctx, stream).cuda_stream))
+    return values, tokens, lse
+
+
+def _distill_rows(ctx, logits, values, tokens, lse, temperature):
+    _on(ctx, logits, values, tokens, lse)
+    ptr, stride = _rows_of(logits)
+    rows, V = logits.shape
+    if values.dim() != 2:
+        raise ValueError("values must be [rows, k]")
+    k = values.shape[1]
+    return _DistillRows(ptr, _row_dtype(logits), stride, _shaped(values, (rows, k), torch.float32),
+                        _shaped(tokens, (rows, k), torch.int32), _shaped(lse, (rows,), torch.float32), rows, V, k,
+                        float(temperature))
+
+
+def _gradient(ctx, stream, logits, grad):
+    if grad is None:
+        grad = _empty(ctx, stream, tuple(logits.shape), logits.dtype)
+    _on(ctx, grad)
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("the gradient must have the shape and type of the logits")
+    return grad, *_rows_of(grad)
+
+
+def specdec_distill(ctx: Context, logits, values, tokens, lse, temperature: float = 1.0, loss=None, saved=None,
+                    stream=None):
+    """specdec_distill of the C ABI: draft logits [rows, V] against the target's record (values, tokens [rows, k]; lse
+    [rows], or None to renormalise over the list) -> (loss [rows] f32, saved for specdec_distill_backward)."""
+    r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
+    _on(ctx, loss, saved)
+    if loss is None:
+        loss = _empty(ctx, stream, (r.rows,), torch.float32)
+    if saved is None:
+        saved = _empty(ctx, stream, (r.rows, DISTILL_SAVED), torch.float32)
+    ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), _shaped(loss, (r.rows,), torch.float32),
+                                       _shaped(saved, (r.rows, DISTILL_SAVED), torch.float32),
+                                       _row_stream(ctx, stream).cuda_stream))
+    return loss, saved
+
+
+def specdec_distill_backward(ctx: Context, logits, values, tokens, lse, saved, row_grad, temperature: float = 1.0,
+                             grad=None, stream=None):
+    """specdec_distill_backward of the C ABI: gradient [rows, V] of sum_n row_grad[n] * loss[n] in the draft logits, of
+    their type; `grad` may be `logits` itself."""
+    r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
+    _on(ctx, saved, row_grad)
+    grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
+    ctx._check(ctx.lib.specdec_distill_backward(ctx.handle, C.byref(r), _shaped(saved, (r.rows, DISTILL_SAVED), torch.float32),
+                                                _shaped(row_grad, (r.rows,), torch.float32), gptr, gstride,
+                                                _row_stream(ctx, stream).cuda_stream))
+    return grad
+
+
+def specdec_distill_step(ctx: Context, logits, values, tokens, lse, row_weight, temperature: float = 1.0, loss=None,
+                         grad=None, stream=None):
+    """specdec_distill_step of the C ABI: (loss [rows], gradient [rows, V] of sum_n row_weight[n] * loss[n]) in one pass;
+    `grad` may be `logits` itself."""
+    r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
+    _on(ctx, row_weight, loss)
+    if loss is None:
+        loss = _empty(ctx, stream, (r.rows,), torch.float32)
+    grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
+    ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _shaped(row_weight, (r.rows,), torch.float32),
+                                            _shaped(loss, (r.rows,), torch.float32), gptr, gstride,
+                                            _row_stream(ctx, stream).cuda_stream))
+    return loss, grad
+
+
+def specdec_beam_select(ctx: Context, logits, scores, n_out: int, temperature: float = 1.0, finished=None,
+                        end_token: int = 0, out_scores=None, parents=None, tokens=None, workspace=None, stream=None):
+    """specdec_beam_select of the C ABI: logits [B, W, V], scores [B, W] f32, finished [B, W] int32 or None ->
+    (scores [B, n_out] f32, parents [B, n_out] int32, tokens [B, n_out] int32).  The workspace (uint8, at least
+    specdec_beam_workspace bytes) is allocated here unless passed in."""
+    _on(ctx, logits, scores, finished, out_scores, parents, tokens, workspace)
+    if logits.dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
+        raise ValueError("logits must be [B, W, V] with adjacent elements in a row")
+    B, W, V = logits.shape
+    M = int(n_out)
+    beam_stride = logits.stride(1) if W > 1 else V
+    batch_stride = logits.stride(0) if B > 1 else V
+    if out_scores is None:
+        out_scores = _empty(ctx, stream, (B, M), torch.float32)
+    if parents is None:
+        parents = _empty(ctx, stream, (B, M), torch.int32)
+    if tokens is None:
+        tokens = _empty(ctx, stream, (B, M), torch.int32)
+    if workspace is None:
+        workspace = _empty(ctx, stream, (ctx.lib.specdec_beam_workspace(B, W, V, M),), torch.uint8)
+    ctx._check(ctx.lib.specdec_beam_select(
+        ctx.handle, logits.data_ptr(), _row_dtype(logits), batch_stride, beam_stride, _shaped(scores, (B, W), torch.float32),
+        _shaped(finished, (B, W), torch.int32), int(end_token), float(temperature), B, W, V, M,
+        _shaped(out_scores, (B, M), torch.float32), _shaped(parents, (B, M), torch.int32), _shaped(tokens, (B, M), torch.int32),
+        _ptr(workspace, torch.uint8), workspace.numel(), _row_stream(ctx, stream).cuda_stream))
+    return out_scores, parents, tokens
+
+
+def _state_layout(t: torch.Tensor, batch_dim: int, step_dim: int | None):
+    """(outer extent, runs, steps, bytes of a step, strides in bytes of outer, batch, beam, run) of a state tensor:
+    dimensions before the batch are the outer extent, those between the beams and the steps the runs; the rest is a
+    step, whose bytes and those of the next follow one another.  Without step_dim a beam's last adjacent dimensions are
+    one step."""
+    n, es = t.dim(), t.element_size()
+    if not 0 <= batch_dim <= n - 2:
+        raise ValueError(f"batch_dim {batch_dim} of a state with {n} dimensions")
+    if step_dim is not None and not batch_dim + 2 <= step_dim < n:
+        raise ValueError(f"step_dim {step_dim} must come after the beams")
+    at = n
+    adjacent = 1                                   # elements that follow one another from dimension `at` on
+    while at > batch_dim + 2 and (t.shape[at - 1] == 1 or t.stride(at - 1) == adjacent):
+        at -= 1
+        adjacent *= t.shape[at]
+    if step_dim is not None:
+        if at > step_dim:
+            raise ValueError("the bytes of a step, and of the steps, must follow one another")
+        at, adjacent = step_dim, 1
+        for d in range(step_dim + 1, n):
+            adjacent *= t.shape[d]
+
+    def fold(dims):                                # several dimensions as one extent at one stride
+        dims = [d for d in dims if t.shape[d] != 1]
+        if not dims:
+            return 1, 0
+        count = t.shape[dims[-1]]
+        for d, inner in zip(reversed(dims[:-1]), reversed(dims[1:])):
+            if t.stride(d) != t.stride(inner) * t.shape[inner]:
+                raise ValueError("dimensions of the state on one side of the beams must fold into one stride")
+            count *= t.shape[d]
+        return count, t.stride(dims[-1]) * es
+
+    outer, outer_stride = fold(range(batch_dim))
+    runs, run_stride = fold(range(batch_dim + 2, at))
+    steps = 1 if step_dim is None else t.shape[step_dim]
+    if max(outer, runs, steps) >= 1 << 31:
+        raise ValueError("an extent of the state exceeds 2^31")
+    return (outer, runs, steps, adjacent * es, outer_stride, t.stride(batch_dim) * es, t.stride(batch_dim + 1) * es, run_stride)
+
+
+def specdec_beam_reorder(ctx: Context, parents, state, batch_dim: int = 0, step_dim: int | None = None, lens=None, out=None,
+                         stream=None):
+    """specdec_beam_reorder of the C ABI: beam m of entry b takes the state of beam parents[b, m] (int32 [B, W], rows may
+    be strided).  `state` has the entries at batch_dim and the beams behind it; with step_dim only the first lens[b]
+    (int32 [B]) steps move.  In place unless `out`, of the same shape and strides, is given.  Returns the reordered state."""
+    dst = state if out is None else out
+    _on(ctx, parents, state, dst, lens)
+    if dst.shape != state.shape or dst.dtype != state.dtype or dst.stride() != state.stride():
+        raise ValueError("out must have the shape, strides and type of the state")
+    if state.numel() == 0:
+        raise ValueError("the state is empty")
+    layout = _state_layout(state, batch_dim, step_dim)
+    B, W = state.shape[batch_dim], state.shape[batch_dim + 1]
+    if tuple(parents.shape) != (B, W) or parents.dtype != torch.int32 or (W > 1 and parents.stride(1) != 1):
+        raise ValueError(f"parents must be int32 [{B}, {W}] with adjacent beams")
+    if lens is not None and step_dim is None:
+        raise ValueError("lens needs step_dim")
+    st = _BeamState(state.data_ptr(), dst.data_ptr(), *layout)
+    ctx._check(ctx.lib.specdec_beam_reorder(ctx.handle, parents.data_ptr(), parents.stride(0) if B > 1 else W,
+                                            _shaped(lens, (B,), torch.int32), B, W, C.byref(st),
+                                            _row_stream(ctx, stream).cuda_stream))
+    return dst

@@ -1,0 +1,548 @@
+"""GPU parity of the row operators -- top logits, distillation, beam selection, state reordering -- against the numpy
+float64 oracle.
+
+Tolerances.  A softmax term is off by at most 2^-22 (ex2.approx) plus the rounding of its exponent t: |t| 2^-24 ln 2
+twice; weighted with the term itself (2^t) that is below 2 * 2^-24 for t in a row's own range, and at most 16 * 2^-23 ln 2
+for a row whose terms all lie 16 binades below its largest.  Sums add 16 roundings of 2^-24 within a thread.  Together a
+sum is off by less than REL = 4e-6 of itself; results round to 32 bits once (2^-24).
+"""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from oracle import rows_oracle as ro  # noqa: E402
+from paper_2405_19715_b200 import specdec  # noqa: E402
+
+REL = 4e-6
+F24 = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}       # half a step relative to the value
+TINY = {"f32": 1e-37, "bf16": 1e-37, "f16": 2.0 ** -25}                # ... and near zero
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = specdec.Context(1, 1)
+    yield c
+    assert c.device_status() == 0
+    c.close()
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _rows(seed, n, V, dtype, pad=0, offset=0, sigma=2.5):
+    """[n, V] logits on the GPU at stride V + pad, `offset` elements into their buffer, NaN around them."""
+    rng = np.random.default_rng(seed)
+    buf = torch.full((offset + n * (V + pad),), float("nan"), dtype=DT[dtype], device="cuda")
+    x = buf[offset:].view(n, V + pad)[:, :V]
+    x.copy_(torch.from_numpy(rng.normal(size=(n, V)).astype(np.float32) * sigma))
+    return x
+
+
+def _check_top(ctx, x, k, T):
+    values, tokens, lse = specdec.specdec_top_logits(ctx, x, k, T)
+    torch.cuda.synchronize()
+    wv, wt, wl = ro.top_logits(_np(x), k, T)
+    np.testing.assert_array_equal(tokens.cpu().numpy(), wt)
+    np.testing.assert_array_equal(_np(values), wv)
+    got = _np(lse)
+    bad = ~np.isfinite(wl)
+    np.testing.assert_array_equal(got[bad], wl[bad])
+    assert np.all(np.abs(got[~bad] - wl[~bad]) <= REL + F24 * np.abs(wl[~bad]))
+    return values, tokens, lse
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,V,k", [(1, 1, 1), (3, 2, 2), (2, 7, 3), (5, 33, 33), (4, 255, 255), (3, 300, 256), (2, 1000, 50), (200, 1000, 7),
+                                   (7, 4099, 64), (33, 32000, 50), (2, 32001, 256), (150, 32003, 5), (3, 128256, 50), (1, 50021, 1)])
+def test_top_logits(ctx, n, V, k, dtype):
+    _check_top(ctx, _rows(n * 1000 + V + k, n, V, dtype), k, 0.75)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 200003), ("bf16", 300007), ("f16", 300007)])
+def test_top_logits_of_rows_longer_than_a_clusters_registers(ctx, dtype, V):
+    x = _rows(3, 3, V, dtype)
+    x[1] = torch.sort(x[1].float())[0].to(x.dtype)          # every tile holds larger logits than the one before
+    _check_top(ctx, x, 100, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (3, 5), (8, 0), (13, 2)])
+def test_top_logits_strides_and_alignment(ctx, pad, offset, dtype):
+    for V in (9, 1001, 32000):
+        _check_top(ctx, _rows(V + pad, 9, V, dtype, pad, offset), 9, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [40, 5000, 40001, 140000])
+def test_top_logits_hard_rows(ctx, V, dtype):
+    """Rows that let the first bound through: ordered, constant, masked, with ties, NaN and infinities."""
+    x = _rows(V, 16, V, dtype)
+    low = torch.finfo(x.dtype).min
+    x[0] = torch.sort(x[0].float())[0].to(x.dtype)
+    x[1] = torch.sort(x[1].float(), descending=True)[0].to(x.dtype)
+    x[2] = 0.0
+    x[3] = float("-inf")
+    keep = torch.arange(7, device="cuda") * (V // 7)
+    for row, fill in ((4, float("-inf")), (5, low), (6, float("nan"))):
+        kept = x[row, keep].clone()
+        x[row] = fill
+        x[row, keep] = kept
+    x[7] = torch.where(torch.arange(V, device="cuda") % 2 == 0, 0.0, -0.0).to(x.dtype)     # equal, although their bits are not
+    x[8] = (torch.arange(V, device="cuda") % 3).to(x.dtype)
+    x[9, V // 2] = float("inf")
+    x[10, V - 1] = float("nan")
+    x[11] = float("nan")
+    x[12] = low
+    x[13, : V - 3] = float("-inf")
+    x[14, 3:] = float("-inf")
+    x[14, 5] = float("nan")
+    x[15] = -x[15].abs() - 1
+    for k in (1, 30, min(V, 256)):
+        _check_top(ctx, x, k, 1.0)
+
+
+def test_top_logits_refusals(ctx):
+    x = torch.zeros(4, 16, device="cuda")
+    for args in ((x, 0), (x, 17), (torch.zeros(1, 400, device="cuda"), 257), (x, 3, 0.0), (x, 3, float("nan")), (x, 3, 1e7)):
+        with pytest.raises(specdec.SpecdecError) as e:
+            specdec.specdec_top_logits(ctx, *args)
+        assert e.value.code == specdec.EINVAL
+    for bad in (x.cpu(), x.double(), x.t(), x[0], x[:, ::2]):
+        with pytest.raises(ValueError):
+            specdec.specdec_top_logits(ctx, bad, 2)
+    with pytest.raises(specdec.SpecdecError):
+        specdec.specdec_top_logits(ctx, x[:1].expand(4, 16), 2)        # stride 0
+    with pytest.raises(ValueError):
+        specdec.specdec_top_logits(ctx, x, 2, values=torch.zeros(4, 3, device="cuda"))
+
+
+# ---- distillation ------------------------------------------------------------------------------------------------------
+
+def _record(seed, n, V, k, dtype, T, rest, pad=0, offset=0):
+    z = _rows(seed, n, V, dtype, pad, offset)
+    rng = np.random.default_rng(seed + 1)
+    t = (z.float() + torch.from_numpy(rng.normal(size=(n, V)).astype(np.float32)).cuda()).contiguous()
+    values, tokens = torch.topk(t, min(k, V), dim=1)
+    lse = torch.logsumexp(t.double() / T, 1).float() if rest else None
+    w = torch.from_numpy(rng.uniform(0.5, 2.0, size=n).astype(np.float32)).cuda()
+    return z, values.contiguous(), tokens.to(torch.int32).contiguous(), lse, w
+
+
+def _check_distill(z, values, tokens, lse, T, w, dtype, loss, grad, weighted_loss=True):
+    zn, vn, tn, ln, wn = _np(z), _np(values), tokens.cpu().numpy(), None if lse is None else _np(lse), _np(w)
+    want_l, want_g = ro.distill(zn, vn, tn, ln, T, wn)
+    if weighted_loss:
+        want_l = np.where(wn == 0, 0.0, want_l)
+    got_l, got_g = _np(loss), _np(grad)
+    np.testing.assert_array_equal(np.isfinite(got_l), np.isfinite(want_l))
+    np.testing.assert_array_equal(got_l[~np.isfinite(want_l)], want_l[~np.isfinite(want_l)])
+    fin = np.isfinite(want_l)
+    # sum p log S, and R log Q twice, each off by REL; the terms themselves are in 64 bits
+    assert np.all(np.abs(got_l[fin] - want_l[fin]) <= 3 * REL + F24 * np.abs(want_l[fin])), np.abs(got_l[fin] - want_l[fin]).max()
+    np.testing.assert_array_equal(np.isnan(got_g), np.isnan(want_g))
+    for n in range(len(zn)):
+        if np.isnan(want_g[n]).any() or not want_g[n].any():
+            np.testing.assert_array_equal(got_g[n], want_g[n])
+            continue
+        # q is off by REL of itself (its term and its sum), R/Q by REL, p by the rounding to 32 bits; then one rounding to the type
+        q = np.exp(ro.log_softmax(zn[n], T))
+        y = tn[n][tn[n] >= 0]
+        out = np.ones(len(q), bool)
+        out[y] = False
+        Q = q[out].sum()
+        p = np.zeros(len(q))
+        norm = ln[n] if ln is not None else ro.log_sum_exp(vn[n][tn[n] >= 0], T)
+        p[y] = np.exp(vn[n][tn[n] >= 0] / T - norm)
+        R = max(0.0, 1 - p.sum()) if ln is not None and Q > 0 else 0.0
+        scale = abs(wn[n]) / T * (q * (p.sum() + R + (R / Q if R > 0 else 0.0)) * 2 * REL + p * 2 * F24)
+        tol = scale + HALF[dtype] * (np.abs(want_g[n]) + scale) + TINY[dtype]
+        over = np.abs(got_g[n] - want_g[n]) - tol
+        assert np.all(over <= 0), (n, over.argmax(), over.max(), got_g[n][over.argmax()], want_g[n][over.argmax()])
+
+
+def _run_all(ctx, z, values, tokens, lse, w, T, dtype):
+    loss, grad = specdec.specdec_distill_step(ctx, z, values, tokens, lse, w, T)
+    loss1, saved = specdec.specdec_distill(ctx, z, values, tokens, lse, T)
+    grad1 = specdec.specdec_distill_backward(ctx, z, values, tokens, lse, saved, w, T)
+    torch.cuda.synchronize()
+    _check_distill(z, values, tokens, lse, T, w, dtype, loss, grad)
+    _check_distill(z, values, tokens, lse, T, w, dtype, loss1, grad1, weighted_loss=False)
+    return loss, grad
+
+
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,V,k,T", [(1, 1, 1, 1.0), (2, 2, 1, 0.5), (3, 7, 7, 1.0), (4, 33, 5, 2.0), (3, 1000, 1000, 1.0), (170, 999, 16, 1.25),
+                                     (5, 4099, 64, 1.0), (40, 32000, 50, 1.0), (2, 50021, 256, 2.0), (3, 128256, 64, 0.75)])
+def test_distill(ctx, n, V, k, T, dtype, rest):
+    z, values, tokens, lse, w = _record(n + V + k, n, V, k, dtype, T, rest)
+    _run_all(ctx, z, values, tokens, lse, w, T, dtype)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 150001), ("bf16", 270001)])
+def test_distill_of_rows_longer_than_a_clusters_registers(ctx, dtype, V):
+    z, values, tokens, lse, w = _record(9, 3, V, 40, dtype, 1.0, True)
+    z[1] = torch.sort(z[1].float())[0].to(z.dtype)
+    loss, grad = _run_all(ctx, z, values, tokens, lse, w, 1.0, dtype)
+    zz = z.clone()
+    assert torch.equal(specdec.specdec_distill_step(ctx, zz, values, tokens, lse, w, 1.0, grad=zz)[1], grad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("pad,offset,gpad,goffset", [(0, 1, 0, 1), (3, 5, 3, 5), (1, 0, 0, 0), (5, 2, 9, 3)])
+def test_distill_strides_and_alignment(ctx, pad, offset, gpad, goffset, dtype):
+    """Logits and gradient at different strides and offsets; what lies around the gradient stays as it was."""
+    for n, V in ((9, 31), (5, 4099)):
+        z, values, tokens, lse, w = _record(V + pad, n, V, 20, dtype, 1.0, True, pad, offset)
+        buf = torch.full((goffset + n * (V + gpad),), 77.0, dtype=DT[dtype], device="cuda")
+        g = buf[goffset:].view(n, V + gpad)[:, :V]
+        loss, grad = specdec.specdec_distill_step(ctx, z, values, tokens, lse, w, 1.0, grad=g)
+        _, saved = specdec.specdec_distill(ctx, z, values, tokens, lse, 1.0)
+        torch.cuda.synchronize()
+        _check_distill(z, values, tokens, lse, 1.0, w, dtype, loss, grad)
+        first = g.clone()
+        specdec.specdec_distill_backward(ctx, z, values, tokens, lse, saved, w, 1.0, grad=g)
+        torch.cuda.synchronize()
+        _check_distill(z, values, tokens, lse, 1.0, w, dtype, loss, g)
+        g.fill_(77.0)
+        assert torch.all(buf == 77.0)
+        # on the logits themselves: the same alignment, and so the same bits
+        zz = torch.empty(offset + n * (V + pad), dtype=DT[dtype], device="cuda")[offset:].view(n, V + pad)[:, :V]
+        zz.copy_(z)
+        assert torch.equal(specdec.specdec_distill_step(ctx, zz, values, tokens, lse, w, 1.0, grad=zz)[1], first)
+        zz.copy_(z)
+        a = specdec.specdec_distill_backward(ctx, z, values, tokens, lse, saved, w, 1.0)
+        assert torch.equal(specdec.specdec_distill_backward(ctx, zz, values, tokens, lse, saved, w, 1.0, grad=zz), a)
+
+
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [600, 40001])
+def test_distill_hard_rows(V, dtype, rest):
+    ctx = specdec.Context(1, 1)
+    k = 12
+    z, values, tokens, lse, w = _record(V, 16, V, k, dtype, 1.0, rest)
+    low = torch.finfo(z.dtype).min
+    everything = torch.arange(V, device="cuda")
+    outside = torch.ones(16, V, dtype=torch.bool, device="cuda").scatter_(1, tokens.long(), False)
+    z[0][outside[0]] = float("-inf")                 # the draft has nothing outside the list
+    z[1][outside[1]] = low                           # a mask of the type's lowest value
+    z[2][tokens[2, 0].long()] = float("-inf")        # a listed token that the draft rules out: loss +inf
+    z[3] = float("-inf")                             # a mask that leaves nothing
+    z[4, V // 3] = float("nan")
+    z[5, V // 3] = float("inf")
+    tokens[6] = -1                                   # padding
+    z[6] = float("nan")
+    tokens[7, 5:] = -1                               # a shorter list
+    values[8] = float("-inf")                        # the target has no mass on the list
+    values[9, 3:] = float("-inf")
+    tokens[10, 4] = tokens[10, 7]                    # listed twice
+    tokens[11, 2] = V                                # no token
+    tokens[12, 1] = -2
+    w[13] = 0.0
+    z[13] = float("nan")
+    z[14] = low
+    z[15] = (everything % 5).to(z.dtype)
+    w[1] = -3.0
+    loss, grad = _run_all(ctx, z, values, tokens, lse, w, 1.0, dtype)
+    assert torch.all(grad[13] == 0) and loss[13] == 0 and torch.all(grad[6] == 0) and loss[6] == 0
+    assert ctx.device_status() == specdec.DATA_BAD_TOKEN
+    assert ctx.device_status() == 0
+    ctx.close()
+
+
+def test_distill_gradient_against_differences_of_the_kernels_loss(ctx):
+    """fp32 logits, T = 1: the loss falls by the gradient along its own direction.  With a step h the difference quotient
+    is off by h^2 times a third derivative (at most 1 here) and by two losses' rounding of 4 REL over 2 h."""
+    z, values, tokens, lse, w = _record(21, 6, 777, 30, "f32", 1.0, True)
+    loss, saved = specdec.specdec_distill(ctx, z, values, tokens, lse, 1.0)
+    g = specdec.specdec_distill_backward(ctx, z, values, tokens, lse, saved, torch.ones_like(w), 1.0)
+    h = 0.02
+    d = g / g.norm(dim=1, keepdim=True)
+    up, _ = specdec.specdec_distill(ctx, z + h * d, values, tokens, lse, 1.0)
+    down, _ = specdec.specdec_distill(ctx, z - h * d, values, tokens, lse, 1.0)
+    num = (up - down).double() / (2 * h)
+    want = (g.double() * d.double()).sum(1)
+    assert torch.all((num - want).abs() <= h * h + 4 * REL / h)
+
+
+def test_distill_refusals(ctx):
+    z, values, tokens, lse, w = _record(4, 4, 100, 8, "bf16", 1.0, True)
+    with pytest.raises(ValueError):
+        specdec.specdec_distill(ctx, z.cpu(), values, tokens, lse)
+    with pytest.raises(ValueError):
+        specdec.specdec_distill(ctx, z, values, tokens.long(), lse)
+    with pytest.raises(ValueError):
+        specdec.specdec_distill(ctx, z, values, tokens[:, :4].contiguous(), lse)
+    with pytest.raises(ValueError):
+        specdec.specdec_distill_step(ctx, z, values, tokens, lse, w, grad=torch.zeros(4, 100, device="cuda"))
+    buf = torch.zeros(1000, dtype=torch.bfloat16, device="cuda")
+    zz, g = buf[:400].view(4, 100), buf[8:408].view(4, 100)
+    for bad in (dict(grad=g), ):
+        with pytest.raises(specdec.SpecdecError) as e:
+            specdec.specdec_distill_step(ctx, zz, values, tokens, lse, w, **bad)
+        assert e.value.code == specdec.EINVAL
+    with pytest.raises(specdec.SpecdecError):
+        specdec.specdec_distill(ctx, z, values, tokens, lse, -1.0)
+    big = torch.zeros(4, 1025, device="cuda")
+    with pytest.raises(specdec.SpecdecError):
+        specdec.specdec_distill(ctx, z, big, big.to(torch.int32), lse)
+
+
+# ---- beams -------------------------------------------------------------------------------------------------------------
+
+def _check_beam(ctx, x, scores, M, T, finished=None, end=0):
+    """Exact order, but for candidates whose scores lie within 2 REL of one another (none is expected)."""
+    s, p, t = specdec.specdec_beam_select(ctx, x, scores, M, T, finished=finished, end_token=end)
+    torch.cuda.synchronize()
+    xn, sn, fn = _np(x), _np(scores), None if finished is None else finished.cpu().numpy()
+    ws, wp, wt = ro.beam_select(xn, sn, M, T, fn, end)
+    s, p, t = _np(s), p.cpu().numpy(), t.cpu().numpy()
+    V = x.shape[2]
+    for b in range(x.shape[0]):
+        if np.array_equal(p[b], wp[b]) and np.array_equal(t[b], wt[b]):
+            continue
+        c = ro.beam_scores(xn[b], sn[b], T, None if fn is None else fn[b], end)
+        picked = [(int(a), int(v)) for a, v in zip(p[b], t[b])]
+        assert len(set(picked)) == len(picked)
+        for i, (a, v) in enumerate(picked):
+            assert abs(c[a, v] - ws[b, i]) <= 2 * REL, (b, i, a, v, c[a, v], ws[b, i])
+    fin = np.isfinite(ws)
+    np.testing.assert_array_equal(np.isneginf(s), ~fin)
+    assert np.all(np.abs(s - np.where(fin, ws, 0))[fin] <= REL + F24 * np.abs(ws[fin]))
+    return s, p, t
+
+
+def _beams(seed, B, W, V, dtype):
+    x = _rows(seed, B * W, V, dtype).view(B, W, V)
+    scores = torch.from_numpy(np.random.default_rng(seed + 5).normal(size=(B, W)).astype(np.float32) * 2 - 9).cuda()
+    return x, scores
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,W,V,M,T", [(1, 1, 1, 1, 1.0), (2, 3, 2, 6, 1.0), (1, 1, 5000, 256, 1.0), (3, 4, 33, 8, 0.5), (1, 4, 32000, 8, 1.0), (5, 16, 1001, 32, 0.75),
+                                       (2, 64, 500, 128, 1.0), (40, 5, 4099, 10, 2.0), (2, 8, 128256, 16, 1.0), (1, 128, 300, 64, 1.0)])
+def test_beam_select(ctx, B, W, V, M, T, dtype):
+    x, scores = _beams(B + W + V, B, W, V, dtype)
+    _check_beam(ctx, x, scores, M, T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [5, 40, 3001])
+def test_beam_select_hard_beams(ctx, V, dtype):
+    B, W = 8, 6
+    x, scores = _beams(V, B, W, V, dtype)
+    fin = torch.zeros(B, W, dtype=torch.int32, device="cuda")
+    scores[0, 1:] = float("-inf")                    # the first step of a search: one beam
+    scores[1] = float("-inf")                        # nothing at all
+    fin[2] = 1                                       # every beam has ended
+    fin[3, ::2] = -5
+    x[3, ::2] = float("nan")                         # rows of ended beams are not looked at
+    x[4, 2] = float("-inf")                          # a mask that leaves nothing
+    x[4, 3, 1:] = float("-inf")                      # ... and one that leaves a token
+    x[5, 0, 2] = float("nan")
+    x[5, 1, 2] = float("inf")
+    x[6] = 1.0                                       # ties within every beam, and between beams of the same score
+    scores[6, :3] = -4.0
+    scores[6, 3:] = -5.0
+    scores[7, 0] = float("nan")
+    scores[7, 1] = float("inf")
+    fin[7, 2] = 1
+    scores[7, 2] = float("nan")
+    for M in (1, min(12, W * V), min(W * V, 200)):
+        _check_beam(ctx, x, scores, M, 1.0, fin, end=V - 1)
+
+
+def test_beam_select_strides(ctx):
+    B, W, V = 3, 4, 1003
+    buf = torch.full((W + 1, B, V + 5), float("nan"), dtype=torch.bfloat16, device="cuda")
+    x = buf[:W, :, 1:V + 1].transpose(0, 1)          # beams apart by more than the entries, rows at odd addresses
+    src, scores = _beams(8, B, W, V, "bf16")
+    x.copy_(src)
+    _check_beam(ctx, x, scores, 9, 1.0)
+
+
+def test_beam_select_refusals(ctx):
+    x, scores = _beams(1, 2, 4, 50, "bf16")
+    for M in (0, 257, 201):
+        with pytest.raises(specdec.SpecdecError) as e:
+            specdec.specdec_beam_select(ctx, x, scores, M)
+        assert e.value.code == specdec.EINVAL
+    with pytest.raises(specdec.SpecdecError) as e:
+        specdec.specdec_beam_select(ctx, x, scores, 4, finished=torch.zeros(2, 4, dtype=torch.int32, device="cuda"), end_token=50)
+    assert e.value.code == specdec.EINVAL
+    with pytest.raises(specdec.SpecdecError):
+        specdec.specdec_beam_select(ctx, x, scores, 4, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+    wide, s = _beams(1, 1, 100, 300, "bf16")
+    with pytest.raises(specdec.SpecdecError) as e:
+        specdec.specdec_beam_select(ctx, wide, s, 100)
+    assert e.value.code == specdec.EUNSUPPORTED
+    for args in ((x, scores.double(), 4), (x, scores[:, :3].contiguous(), 4), (x[0], scores, 4), (x, scores.cpu(), 4)):
+        with pytest.raises(ValueError):
+            specdec.specdec_beam_select(ctx, *args)
+
+
+def _ints(seed, shape, dtype):
+    rng = np.random.default_rng(seed)
+    return torch.from_numpy(rng.integers(0, 120, size=shape).astype(np.int64)).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.int16, torch.float32, torch.int64])
+@pytest.mark.parametrize("B,W,S,D", [(1, 1, 1, 1), (2, 2, 5, 3), (3, 4, 17, 33), (2, 7, 100, 64), (2, 16, 9, 128), (1, 17, 33, 5), (2, 40, 50, 24), (1, 128, 21, 16)])
+def test_beam_reorder(ctx, B, W, S, D, dtype, in_place):
+    state = _ints(B + W + S, (B, W, S, D), dtype)
+    parents = torch.from_numpy(np.random.default_rng(W).integers(-1, W, size=(B, W)).astype(np.int32)).cuda()
+    lens = torch.tensor([S // 2, S + 4, -3][:B], dtype=torch.int32).cuda()
+    for ln in (None, lens):
+        want = ro.beam_reorder(state.cpu().numpy(), parents.cpu().numpy(), None if ln is None else ln.cpu().numpy())
+        st = state.clone()
+        if in_place:
+            got = specdec.specdec_beam_reorder(ctx, parents, st, step_dim=2, lens=ln)
+            assert got is st
+        else:
+            out = torch.full_like(st, 99)
+            got = specdec.specdec_beam_reorder(ctx, parents, st, step_dim=2, lens=ln, out=out)
+            assert torch.equal(st, state)
+            if ln is not None:                       # steps beyond the length are left as they were in out
+                for b in range(B):
+                    want[b, :, max(0, min(int(ln[b]), S)):] = 99
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(got.cpu().numpy(), want)
+
+
+def test_beam_reorder_layouts(ctx):
+    """Caches with layers in front and heads between beams and steps, prefixes of larger buffers, odd addresses."""
+    L, B, W, H, S, D = 3, 2, 5, 4, 12, 10
+    parents2 = torch.from_numpy(np.random.default_rng(4).integers(0, W, size=(B, 2 * W)).astype(np.int32)).cuda()
+    parents = parents2[:, :W]                        # the first W of 2 W selected: strided rows
+    lens = torch.tensor([7, 12], dtype=torch.int32).cuda()
+    cache = _ints(5, (L, B, W, H, S, D), torch.int16)
+    want = cache.cpu().numpy().copy()
+    for l in range(L):
+        for h in range(H):
+            want[l, :, :, h] = ro.beam_reorder(want[l, :, :, h], parents.cpu().numpy(), lens.cpu().numpy())
+    keep = cache.clone()
+    specdec.specdec_beam_reorder(ctx, parents, cache, batch_dim=1, step_dim=4, lens=lens)
+    np.testing.assert_array_equal(cache.cpu().numpy(), want)
+    cache.copy_(keep)
+    specdec.specdec_beam_reorder(ctx, parents, cache[:, :, :, :, :7], batch_dim=1, step_dim=4)      # a view of the first steps
+    for l in range(L):
+        for h in range(H):
+            part = keep[l, :, :, h].cpu().numpy()
+            np.testing.assert_array_equal(cache[l, :, :, h].cpu().numpy(), ro.beam_reorder(part, parents.cpu().numpy(), [7, 7]))
+    odd = torch.zeros(1 + B * W * 35, dtype=torch.uint8, device="cuda")[1:].view(B, W, 35)
+    odd.copy_(_ints(6, (B, W, 35), torch.uint8))
+    want = ro.beam_reorder(odd.cpu().numpy(), parents.cpu().numpy())
+    specdec.specdec_beam_reorder(ctx, parents, odd)
+    np.testing.assert_array_equal(odd.cpu().numpy(), want)
+
+
+def test_beam_reorder_bad_parent_and_refusals():
+    ctx = specdec.Context(1, 1)
+    st = _ints(1, (2, 4, 6), torch.int32)
+    parents = torch.tensor([[0, 4, 1, 0], [1, 1, 1, 1]], dtype=torch.int32).cuda()
+    want = ro.beam_reorder(st.cpu().numpy(), parents.cpu().numpy())
+    specdec.specdec_beam_reorder(ctx, parents, st)
+    assert ctx.device_status() == specdec.DATA_BAD_PARENT
+    np.testing.assert_array_equal(st.cpu().numpy(), want)
+    with pytest.raises(specdec.SpecdecError) as e:
+        specdec.specdec_beam_reorder(ctx, parents, st[:, :1].expand(2, 4, 6))
+    assert e.value.code == specdec.EINVAL
+    buf = torch.zeros(100, dtype=torch.int32, device="cuda")
+    with pytest.raises(specdec.SpecdecError) as e:
+        specdec.specdec_beam_reorder(ctx, parents, buf[:48].view(2, 4, 6), out=buf[4:52].view(2, 4, 6))
+    assert e.value.code == specdec.EINVAL
+    wide = torch.zeros(1, 129, 4, device="cuda")
+    with pytest.raises(specdec.SpecdecError) as e:
+        specdec.specdec_beam_reorder(ctx, torch.zeros(1, 129, dtype=torch.int32, device="cuda"), wide)
+    assert e.value.code == specdec.EUNSUPPORTED
+    for bad in (dict(parents=parents.long()), dict(parents=parents[:, :3]), dict(lens=torch.zeros(2, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            specdec.specdec_beam_reorder(ctx, **{"parents": parents, "state": st, **bad})
+    assert ctx.device_status() == 0
+    ctx.close()
+
+
+# ---- streams, graphs, and all of them together -------------------------------------------------------------------------
+
+def test_streams_graphs_and_repeats(ctx):
+    """Two streams at once, a captured graph replayed on new inputs, and the same bits every time."""
+    z, values, tokens, lse, w = _record(30, 64, 32000, 50, "bf16", 1.0, True)
+    x, scores = _beams(31, 4, 8, 32000, "bf16")
+
+    def everything(stream=None):
+        a = specdec.specdec_top_logits(ctx, z, 50, 1.0, stream=stream)
+        b = specdec.specdec_distill_step(ctx, z, values, tokens, lse, w, 1.0, stream=stream)
+        c = specdec.specdec_distill(ctx, z, values, tokens, lse, 1.0, stream=stream)
+        d = specdec.specdec_distill_backward(ctx, z, values, tokens, lse, c[1], w, 1.0, stream=stream)
+        e = specdec.specdec_beam_select(ctx, x, scores, 16, 1.0, stream=stream)
+        return [*a, *b, *c, d, *e]
+
+    first = everything()
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    on1, on2 = [], []
+    for _ in range(3):
+        on1, on2 = everything(s1), everything(s2)
+    torch.cuda.synchronize()
+    for a, b, c in zip(first, on1, on2):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = everything()
+    z.copy_(z.flip(0).clone())
+    x.copy_(x.flip(0).clone())
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    want = everything()
+    torch.cuda.synchronize()
+    for a, b in zip(out, want):
+        assert torch.equal(a, b)
+
+
+def test_search_and_training_as_a_program_uses_them(ctx):
+    """A draft searches with beams -- select, reorder the states, extend -- and learns from the target's record; every
+    step against the oracle on the same numbers."""
+    rng = np.random.default_rng(77)
+    B, W, V, d, steps, M = 2, 4, 301, 8, 5, 8
+    emb, out_w = rng.normal(size=(V, d)).astype(np.float32), (rng.normal(size=(d, V)) * 0.7).astype(np.float32)
+    E, O = torch.from_numpy(emb).cuda(), torch.from_numpy(out_w).cuda()
+    hidden = torch.zeros(B, W, d, device="cuda")
+    history = torch.full((B, W, steps), -1, dtype=torch.int32, device="cuda")
+    scores = torch.full((B, W), float("-inf"), device="cuda")
+    scores[:, 0] = 0.0
+    h_ref, hist_ref, s_ref = hidden.cpu().numpy(), history.cpu().numpy(), _np(scores)
+    for t in range(steps):
+        logits = (hidden @ O).contiguous()
+        got = specdec.specdec_beam_select(ctx, logits, scores, M, 1.0)
+        ws, wp, wt = ro.beam_select(_np(logits), s_ref, M, 1.0)
+        np.testing.assert_array_equal(got[1].cpu().numpy(), wp)
+        np.testing.assert_array_equal(got[2].cpu().numpy(), wt)
+        scores = got[0][:, :W].contiguous()
+        s_ref = _np(scores)
+        parents, tok = got[1][:, :W], got[2][:, :W]
+        specdec.specdec_beam_reorder(ctx, parents, hidden)
+        specdec.specdec_beam_reorder(ctx, parents, history, step_dim=2, lens=torch.full((B,), t, dtype=torch.int32, device="cuda"))
+        history[:, :, t] = tok
+        hist_ref = ro.beam_reorder(hist_ref, wp[:, :W], [t] * B)
+        hist_ref[:, :, t] = wt[:, :W]
+        np.testing.assert_array_equal(history.cpu().numpy(), hist_ref)
+        hidden = torch.tanh(hidden + E[tok.long()])
+    # the target's record of the best beams' rows, and a step of the draft's output layer on it
+    rows = hidden.view(B * W, d)
+    target = torch.from_numpy(rng.normal(size=(B * W, V)).astype(np.float32) * 2).cuda()
+    values, tokens, lse = specdec.specdec_top_logits(ctx, target, 20, 1.0)
+    z = (rows @ O).contiguous()
+    weight = torch.full((B * W,), 1.0 / (B * W), device="cuda")
+    loss, grad = specdec.specdec_distill_step(ctx, z, values, tokens, lse, weight, 1.0)
+    torch.cuda.synchronize()
+    _check_distill(z, values, tokens, lse, 1.0, weight, "f32", loss, grad)
+    tok = specdec.specdec_sample(specdec.Context(B * W, 1), (rows @ (O - rows.t() @ grad)).contiguous(), torch.full((B * W,), 0.5, device="cuda"), 1.0)
+    assert torch.all((tok >= 0) & (tok < V))
