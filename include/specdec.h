@@ -434,7 +434,8 @@ typedef struct specdec_distill_rows {
     float temperature;          /* T; of the target's lse as well            */
 } specdec_distill_rows;
 
-/* loss dev out [rows] f32; saved dev out [rows, SPECDEC_DISTILL_SAVED] f32: what specdec_distill_backward needs. */
+/* loss dev out [rows] f32; saved dev out [rows, SPECDEC_DISTILL_SAVED] f32, 16-byte aligned: what specdec_distill_backward
+ * needs. */
 int specdec_distill(specdec_ctx* ctx, const specdec_distill_rows* rows, float* loss, float* saved, void* stream);
 
 /*

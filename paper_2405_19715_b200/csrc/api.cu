@@ -549,14 +549,6 @@ int check_row_args(specdec_ctx* ctx, const char* who, const void* logits, int dt
     if (!(T >= 9.5367431640625e-7f && T <= 1048576.f)) return fail(ctx, SPECDEC_EINVAL, "%s: temperature must be in [2^-20, 2^20]", who);
     return SPECDEC_OK;
 }
-rw::Scale make_scale(double T) {
-    const double c = 1.4426950408889634074 / T;
-    float hi = (float)c;
-    if ((double)hi > c) hi = std::nextafterf(hi, 0.f);
-    const float lo = (float)(c - (double)hi);
-    return rw::Scale{hi, lo > 1e-37f ? lo : 1e-37f};
-}
-
 int distill(specdec_ctx* ctx, const char* who, DistillMode mode, const specdec_distill_rows* r, float* loss, float* saved, const float* weight,
             void* grad, int64_t grad_stride, cudaStream_t s) {
     if (!r || !r->logits || !r->values || !r->tokens) return fail(ctx, SPECDEC_EINVAL, "%s: null pointer argument", who);
@@ -564,6 +556,7 @@ int distill(specdec_ctx* ctx, const char* who, DistillMode mode, const specdec_d
         return fail(ctx, SPECDEC_EINVAL, "%s: null pointer argument", who);
     if (int rc = check_row_args(ctx, who, r->logits, (int)r->dtype, r->row_stride, r->rows, r->V, r->temperature)) return rc;
     if (r->top_k < 1 || r->top_k > SPECDEC_DISTILL_MAX_LIST) return fail(ctx, SPECDEC_EINVAL, "%s: top_k must be in [1, %d] (got %d)", who, SPECDEC_DISTILL_MAX_LIST, r->top_k);
+    if (reinterpret_cast<uintptr_t>(saved) % 16 != 0) return fail(ctx, SPECDEC_EINVAL, "%s: saved must be 16-byte aligned", who);
     if (mode != DistillMode::Loss) {
         const int64_t es = r->dtype == SPECDEC_F32 ? 4 : 2;
         if (grad_stride < r->V) return fail(ctx, SPECDEC_EINVAL, "%s: a gradient row stride of %lld elements, below V=%d", who, (long long)grad_stride, r->V);
@@ -584,7 +577,7 @@ int distill(specdec_ctx* ctx, const char* who, DistillMode mode, const specdec_d
     p.k = r->top_k;
     p.T = (double)r->temperature;
     p.log2e_t = 1.4426950408889634074 / p.T;
-    p.c = make_scale(p.T);
+    p.c = (float)p.log2e_t;
     p.loss = loss;
     p.saved = saved;
     p.weight = weight;
@@ -614,7 +607,7 @@ int specdec_top_logits(specdec_ctx* ctx, const void* logits, specdec_dtype dtype
     p.k = top_k;
     p.T = (double)temperature;
     p.log2e_t = 1.4426950408889634074 / p.T;
-    p.c = make_scale(p.T);
+    p.c = (float)p.log2e_t;
     p.values = values;
     p.tokens = tokens;
     p.lse = lse;
@@ -683,7 +676,7 @@ int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtyp
     t.k = k;
     t.T = (double)temperature;
     t.log2e_t = 1.4426950408889634074 / t.T;
-    t.c = make_scale(t.T);
+    t.c = (float)t.log2e_t;
     t.parts = reinterpret_cast<rw::Part*>(ws);
     t.values = reinterpret_cast<float*>(ws + align_up(rows * sizeof(rw::Part), 256));
     t.tokens = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(t.values) + align_up(rows * k * 4, 256));
@@ -702,7 +695,6 @@ int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtyp
     p.k = k;
     p.M = n_out;
     p.end_token = end_token;
-    p.c = t.c;
     p.T = t.T;
     p.out_scores = out_scores;
     p.out_parents = out_parents;

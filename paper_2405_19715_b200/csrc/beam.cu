@@ -11,6 +11,8 @@ namespace {
 
 using namespace rw;
 
+constexpr int MERGE_THREADS = 512, MERGE_WARPS = MERGE_THREADS / 32;
+
 __device__ __forceinline__ unsigned long long score_key(double s) {
     const unsigned long long b = (unsigned long long)__double_as_longlong(s + 0.0);
     return (b >> 63) ? ~b : (b | 0x8000000000000000ull);
@@ -20,29 +22,22 @@ __device__ __forceinline__ double key_score(unsigned long long key) {
 }
 __device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
 
-__global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
+__global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
     extern __shared__ __align__(16) unsigned char raw[];
     const int n = P.W * P.k;
     unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // 0: no candidate
     int* flat = reinterpret_cast<int*>(keys + n);                               // w * V + v
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int mine = 0;
-    for (int w = warp; w < P.W; w += WARPS) {
+    for (int w = warp; w < P.W; w += MERGE_WARPS) {
         const int row = b * P.W + w;
         const float s = P.scores[row];
         const bool ended = P.finished && P.finished[row], live = s > -INFINITY && s < INFINITY;
         double lse = 0.0;
         bool open = live && !ended;
         if (open) {
-            // lse in 64 bits: the listed terms, the largest of the sum, are exchanged for exact ones
             const Part part = P.parts[row];
-            const float m = reference(part.m);
-            double fix = 0.0;
-            for (int i = lane; i < P.k; i += 32) {
-                const float x = P.values[(size_t)row * P.k + i];
-                fix += exp(((double)x - (double)m) / P.T) - (double)term(x, m, P.c);
-            }
-            lse = (double)m / P.T + log(part.s + warp_sum(fix));
+            lse = (double)reference(part.m) / P.T + log(part.s);
             open = is_finite(lse);                  // a row without a finite sum offers nothing
         }
         for (int i = lane; i < P.k; i += 32) {
@@ -65,10 +60,10 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
         }
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
-    __shared__ int counts[WARPS];
+    __shared__ int counts[MERGE_WARPS];
     if (lane == 0) counts[warp] = mine;
     __syncthreads();
-    for (int i = tid; i < n; i += THREADS) {
+    for (int i = tid; i < n; i += MERGE_THREADS) {
         const unsigned long long key = keys[i];
         if (key == 0) continue;
         const int f = flat[i];
@@ -82,8 +77,8 @@ __global__ void __launch_bounds__(THREADS) beam_merge_kernel(const __grid_consta
         }
     }
     int total = 0;
-    for (int w = 0; w < WARPS; ++w) total += counts[w];
-    for (int i = total + tid; i < P.M; i += THREADS) {          // fewer candidates than places
+    for (int w = 0; w < MERGE_WARPS; ++w) total += counts[w];
+    for (int i = total + tid; i < P.M; i += MERGE_THREADS) {          // fewer candidates than places
         const size_t o = (size_t)b * P.M + i;
         P.out_scores[o] = -INFINITY;
         P.out_parents[o] = -1;
@@ -230,7 +225,7 @@ cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s) {
         const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    beam_merge_kernel<<<B, rw::THREADS, smem, s>>>(p);
+    beam_merge_kernel<<<B, MERGE_THREADS, smem, s>>>(p);
     return cudaGetLastError();
 }
 

@@ -14,44 +14,38 @@
 // the list, and the difference would keep few digits.  A bitmap of the CTA's part of the row tells list from rest.
 // sum p, R and the loss are in 64 bits for the same reason; they are a few values per listed token.
 //
-// A CTA holds up to 4096 16-byte vectors of the row in registers, a cluster of up to 8 CTAs a row; sums meet through
-// distributed shared memory.  The step then forms the gradient from the registers: one read and one write of the row.
-// Longer rows are walked in tiles and read a second time.
+// A row is spread over a cluster of up to 8 CTAs, a warp holding 256 16-byte vectors (4 KB) of it in registers: its terms
+// are summed, the sums of all warps meet through distributed shared memory, and the gradient is formed from the same
+// registers: one read and one write of the row.  Rows that are longer than the cluster's registers are walked in chunks and
+// read a second time.  A listed token belongs to the CTA that has its logit, which adds its part to the sums and corrects
+// its gradient.
+#include <algorithm>
+
 #include "rows.cuh"
 
 namespace {
 
 using namespace rw;
 
-struct DistillShared {
-    double wsum[WARPS], wsum2[WARPS];
-    float wmax[WARPS];
-    double s_out, s_in;                             // this CTA's sums outside and inside the list, against m
-    float m;
-    int bad;
+constexpr int PER_SM = 4;
+
+// What a warp adds to the row's sums.
+struct Record {
+    double e, f, g;                                 // of its listed tokens: sum e, sum e L (see below), sum e (z - z_ref)
+    float s_out, s_in, m;                           // terms outside and inside the list, against m
+    float z_ref;
+    int flags;                                      // 1: a token that is none, or listed twice; 2: the list has an entry
 };
 
-// Sum over the CTA of one double per thread, the same in every thread.  Two barriers: `slot` may be reused at once.
-__device__ __forceinline__ double block_sum(double v, double (&slot)[WARPS], int lane, int warp) {
-    v = warp_sum(v);
-    if (lane == 0) slot[warp] = v;
-    __syncthreads();
-    double s = 0.0;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) s += slot[w];
-    __syncthreads();
-    return s;
-}
-__device__ __forceinline__ float block_max(float v, float (&slot)[WARPS], int lane, int warp) {
-    v = warp_max(v);
-    if (lane == 0) slot[warp] = v;
-    __syncthreads();
-    float m = slot[0];
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) m = fmaxf(m, slot[w]);
-    __syncthreads();
-    return m;
-}
+struct DistillShared {
+    uint4 chunk[NW][CHUNK];
+    Record record[NW];
+    float wmax[NW];
+    // of the row, once the records have met
+    float m, scale;
+    double mass, s, e;
+    int zero;
+};
 
 __device__ __forceinline__ uint32_t store_pair(float a, float b, __nv_bfloat16) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -90,235 +84,316 @@ __device__ __forceinline__ unsigned listed_bits(const uint32_t* bitmap, int j) {
     return (bitmap[bit >> 5] >> (bit & 31)) & ((1u << Row<T>::N) - 1u);
 }
 
+// The same for logits so large that only those equal to the largest count; from memory, rarely.
+template <typename T>
+__device__ __noinline__ void huge_terms(const Slice<T>& S, const uint32_t* bitmap, int j0, float top, int lane, float& s_out, float& s_in) {
+#pragma unroll 1
+    for (int i = 0; i < S.depth; ++i)
+        for (int e = 0; e < Row<T>::N; ++e) {
+            const int j = j0 + i * 32 + lane, v = j * Row<T>::N - S.shift + e;
+            if (j >= S.v1 || v < 0 || v >= S.V) continue;
+            const float t = top == INFINITY ? NAN : huge_term(Row<T>::wide(S.row[v]), top);
+            if (listed_bits<T>(bitmap, j - S.v0) >> e & 1u) s_in += t; else s_out += t;
+        }
+}
+
 template <typename T, DistillMode MODE>
-__global__ void __launch_bounds__(THREADS, 2) distill_kernel(const __grid_constant__ DistillParams P) {
+__global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_constant__ DistillParams P) {
     constexpr int N = Row<T>::N;
     constexpr bool STATS = MODE != DistillMode::Gradient, GRAD = MODE != DistillMode::Loss;
-    __shared__ DistillShared sh;
-    extern __shared__ double dyn[];
-    double* prob = dyn;                             // [k] p; entry i is its thread's alone, here and below
-    int* ids = reinterpret_cast<int*>(prob + P.k);
-    float* zs = reinterpret_cast<float*>(ids + P.k);            // the draft's logits of the listed tokens that this CTA needs
-    uint32_t* bitmap = reinterpret_cast<uint32_t*>(zs + P.k);   // [slice_words] tokens of the list in this CTA's part of the row
-    const int C = P.cluster, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    extern __shared__ __align__(16) unsigned char raw[];
+    DistillShared& sh = *reinterpret_cast<DistillShared*>(raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = P.k, C = P.cluster;
+    // one entry per listed token of this CTA, at the token's place in the list; an entry is its thread's alone
+    double* prob = reinterpret_cast<double*>(raw + sizeof(DistillShared));       // [k] e, then p
+    int* ids = reinterpret_cast<int*>(prob + k);                                 // [k] -1: not of this CTA
+    float* zs = reinterpret_cast<float*>(ids + k);                               // [k]
+    uint32_t* bitmap = reinterpret_cast<uint32_t*>(zs + k);                      // [slice_words] listed tokens of this CTA
     const int row_id = blockIdx.x / C;
     const uint32_t rank = blockIdx.x - row_id * C;
-    const T* row = static_cast<const T*>(P.z) + row_id * P.z_stride;
-    const int V = P.V, k = P.k, shift = row_shift(row), nvec = row_vectors<T>(shift, V);
-    const int per = (nvec + C - 1) / C, v0 = min(nvec, (int)rank * per), v1 = min(nvec, v0 + per);
-    T* grad = GRAD ? static_cast<T*>(P.grad) + row_id * P.g_stride : nullptr;
-    const bool wide = GRAD && row_shift(grad) == shift;
+    const Slice<T> S(static_cast<const T*>(P.z) + row_id * P.z_stride, P.V, C, rank);
+    const int own_steps = S.chunks_of(warp), stride = 32 * S.depth, j_first = S.start(S.first_chunk(warp));
     const float weight = GRAD ? P.weight[row_id] : 1.f;
 
     bool zero = GRAD && weight == 0.f;              // the row takes no part
-    float saved_m = 0.f, saved_s = 1.f, saved_out = 0.f, saved_mass = 0.f;
+    float m = 0.f;
+    double s = 1.0, mass = 0.0;
+    float scale = 0.f;                              // of q's term, outside the list
     if (MODE == DistillMode::Gradient) {
-        const float* sv = P.saved + (size_t)row_id * 4;
-        saved_m = sv[0];
-        saved_s = sv[1];
-        saved_out = sv[2];
-        saved_mass = sv[3];
-        zero |= saved_mass < 0.f;
+        const float4 sv = *reinterpret_cast<const float4*>(P.saved + (size_t)row_id * 4);
+        m = sv.x;
+        s = sv.y;
+        mass = sv.w;
+        zero |= sv.w < 0.f;
+        scale = (float)((double)weight / P.T * (double)sv.z / s);
     }
-    uint4 r[NV];
-    if (!zero) load_tile<T>(row, shift, V, v0, v1, tid, r);     // on its way while the list is read
+    if (!zero && own_steps > 0) S.fetch(j_first, lane, sh.chunk[warp]);        // on its way while the list is read
 
-    // ---- the list
-    bool any = false;
-    int bad = 0;
-    double mass_p = 0.0, plogp = 0.0;               // sum p, sum p log p
+    // ---- the list: e = exp(L), L = v/T - lse, or (v - the largest v)/T to be divided by the sum
+    double e_sum = 0.0, f_sum = 0.0;
+    int flags = 0;
     if (!zero) {
         if (STATS)
-            for (int i = tid; i < P.slice_words; i += THREADS) bitmap[i] = 0;
-        float vmax = -INFINITY;
-        for (int i = tid; i < k; i += THREADS) {
-            const int id = P.tokens[(size_t)row_id * k + i];
-            const bool in = id >= 0 && id < V;
-            bad |= id >= V || id < -1;
-            any |= in;
-            ids[i] = in ? id : -1;
-            if (in) vmax = fmaxf(vmax, P.values[(size_t)row_id * k + i]);
-        }
-        any = __syncthreads_or(any);                // the bitmap is empty, too
+            for (int i = tid; i < P.slice_words; i += NT) bitmap[i] = 0;
         double norm;
         if (P.lse) {
             norm = (double)P.lse[row_id];
+            if (STATS) __syncthreads();             // the bitmap is empty
         } else {
-            const float top = block_max(vmax, sh.wmax, lane, warp);
-            double e = 0.0;
-            for (int i = tid; i < k; i += THREADS) {
-                const float v = P.values[(size_t)row_id * k + i];
-                if (ids[i] >= 0 && v != -INFINITY) e += exp(((double)v - (double)top) / P.T);
-            }
-            norm = (double)top / P.T + log(block_sum(e, sh.wsum, lane, warp));
+            float v_max = -INFINITY;
+            for (int i = tid; i < k; i += NT)
+                if ((unsigned)P.tokens[(size_t)row_id * k + i] < (unsigned)P.V) v_max = fmaxf(v_max, P.values[(size_t)row_id * k + i]);
+            v_max = warp_max(v_max);
+            if (lane == 0) sh.wmax[warp] = v_max;
+            __syncthreads();
+            for (int w = 0; w < NW; ++w) v_max = fmaxf(v_max, sh.wmax[w]);
+            norm = (double)v_max / P.T;
         }
-        for (int i = tid; i < k; i += THREADS) {
-            const int id = ids[i];
-            if (id < 0) continue;
-            const int at = (id + shift) / N;
-            const bool own = at >= v0 && at < v1;
-            if (STATS && own) {
-                const int bit = id + shift - v0 * N;
-                bad |= (atomicOr(&bitmap[bit >> 5], 1u << (bit & 31)) >> (bit & 31)) & 1u;   // a token listed twice
-            }
+        for (int i = tid; i < k; i += NT) {
+            const int id = P.tokens[(size_t)row_id * k + i];
+            const bool in = id >= 0 && id < P.V;
+            const int at = (id + S.shift) / N;      // its vector
+            const bool own = in && at >= S.v0 && at < S.v1;
+            flags |= (in ? 2 : 0) | (id >= P.V || id < -1 ? 1 : 0);
+            ids[i] = own ? id : -1;
+            // a renormalised gradient needs the whole list's sum, and has no other CTA to ask
+            if (!own && !(MODE == DistillMode::Gradient && !P.lse && in)) continue;
             const float v = P.values[(size_t)row_id * k + i];
-            const double log_p = (double)v / P.T - norm, p = v == -INFINITY ? 0.0 : exp(log_p);
-            prob[i] = p;
-            if (own || (STATS && rank == 0)) zs[i] = Row<T>::wide(row[id]);
-            if (p != 0.0) {
-                mass_p += p;
-                plogp += p * log_p;
+            const double L = (double)v / P.T - norm, e = v == -INFINITY ? 0.0 : exp(L);
+            e_sum += e;
+            if (e != 0.0) f_sum += e * L;           // not 0 * -inf
+            if (!own) continue;
+            prob[i] = e;
+            if (STATS) {
+                const int bit = id + S.shift - S.v0 * N;
+                flags |= (atomicOr(&bitmap[bit >> 5], 1u << (bit & 31)) >> (bit & 31)) & 1u;       // listed twice
             }
         }
     }
+    uint4 r[NV];
+    chunk_wait();
+    __syncthreads();                                // the bitmap is complete, and every warp's chunk is there
+#pragma unroll
+    for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
+    if (!zero)
+        for (int i = tid; i < k; i += NT)
+            if (const int id = ids[i]; id >= 0) {
+                const int e = id + S.shift - S.v0 * N;
+                zs[i] = Row<T>::wide(S.steps() == 1 ? reinterpret_cast<const T*>(sh.chunk)[e / (stride * N) * (CHUNK * N) + e % (stride * N)] : S.row[id]);
+            }
 
-    // ---- the draft's sums
-    double S = 1.0, f_out = 0.0, mass = 0.0;
-    float M = 0.f;
+    if (MODE == DistillMode::Gradient && S.steps() > 1) __syncthreads();       // the gradient may lie on the logits
     if (STATS && !zero) {
-        const f2 hi2 = sd::pack2(P.c.hi, P.c.hi), lo2 = sd::pack2(P.c.lo, P.c.lo);
-        double s_out = 0.0, s_in = 0.0;             // of this thread, against run_m
-        float run_m = -INFINITY;
-        for (int t0 = v0; t0 < v1; t0 += TILE) {
-            if (t0 != v0) load_tile<T>(row, shift, V, t0, v1, tid, r);
-            float m = -INFINITY;
+        // ---- the draft's terms
+        float s_out = 0.f, s_in = 0.f, top = -INFINITY;
+        int j0 = j_first;
+        for (int step = 0; step < own_steps; ++step, j0 += stride) {
+            if (step > 0) {
+                S.fetch(j0, lane, sh.chunk[warp]);
+                chunk_wait();
 #pragma unroll
-            for (int i = 0; i < NV; ++i) m = fmaxf(m, vec_max(r[i], T()));        // NaN is skipped here, and met in the sum
-            const float tm = block_max(m, sh.wmax, lane, warp);                   // the bitmap is complete, too
-            const float ref = reference(tm);
-            const f2 neg = sd::pack2(-ref, -ref);
-            f2 acc = sd::pack2(0.f, 0.f);
-            float in = 0.f;
+                for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
+            }
+            Max<T> mx{r[0]};
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                f2 x[N / 2];
-                pairs(r[i], x, T());
-                const int j = t0 + i * THREADS + tid;
-                const unsigned bits = j < v1 ? listed_bits<T>(bitmap, j - v0) : 0u;
-                if (bits == 0u) {
-                    acc = sd::add2(acc, terms<N / 2>(x, neg, hi2, lo2));
-                } else {
-                    float out = 0.f;
+            for (int i = 1; i < NV; ++i) mx = Max<T>{mx, Max<T>{r[i]}};
+            const float own = mx.value(), wm = warp_max(own == own ? own : -INFINITY);    // NaN is met in the sums
+            if (wm > top) {
+                const float f = move_terms(top, wm, P.c);            // the sums are 0 so far where top is -inf
+                s_out *= f;
+                s_in *= f;
+                top = wm;
+            }
+            if (ordinary(top) || top == -INFINITY) {
+                const float u = reference(top) * P.c;
+                const f2 neg = sd::pack2(-u, -u), c2 = sd::pack2(P.c, P.c);
+                f2 acc = sd::pack2(0.f, 0.f);
+                float in = 0.f;
 #pragma unroll
-                    for (int q = 0; q < N / 2; ++q) {
-                        float a, b;
-                        sd::unpack2(term2(x[q], neg, hi2, lo2), a, b);
-                        if (bits >> (2 * q) & 1u) in += a; else out += a;
-                        if (bits >> (2 * q + 1) & 1u) in += b; else out += b;
+                for (int i = 0; i < NV; ++i) {
+                    f2 x[N / 2];
+                    pairs(r[i], x, T());
+                    const unsigned bits = i < S.depth ? listed_bits<T>(bitmap, min(j0 + i * 32 + lane, S.v1 - 1) - S.v0) : 0u;
+                    if (bits == 0u) {
+                        acc = sd::add2(acc, terms<N / 2>(x, c2, neg));
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < N / 2; ++q) {
+                            float a, b;
+                            sd::unpack2(term2(x[q], c2, neg), a, b);
+                            const bool la = bits >> (2 * q) & 1u, lb = bits >> (2 * q + 1) & 1u;
+                            in += (la ? a : 0.f) + (lb ? b : 0.f);
+                            acc = sd::add2(acc, sd::pack2(la ? 0.f : a, lb ? 0.f : b));
+                        }
                     }
-                    acc = sd::add2(acc, sd::pack2(out, 0.f));
                 }
-            }
-            const float to = fmaxf(run_m, tm);
-            const double f0 = rescale(run_m, to, P.log2e_t), f1 = rescale(tm, to, P.log2e_t);
-            s_out = s_out * f0 + (double)fold2(acc) * f1;
-            s_in = s_in * f0 + (double)in * f1;
-            run_m = to;
-        }
-        s_out = block_sum(s_out, sh.wsum, lane, warp);
-        s_in = block_sum(s_in, sh.wsum, lane, warp);
-        bad = __syncthreads_or(bad);
-        M = run_m;
-        if (C > 1) {
-            if (tid == 0) {
-                sh.s_out = s_out;
-                sh.s_in = s_in;
-                sh.m = run_m;
-                sh.bad = bad;
-            }
-            sd::cl_sync();
-            for (int q = 0; q < C; ++q) M = fmaxf(M, cl_ld_f32(&sh.m, q));
-            s_out = s_in = 0.0;
-            for (int q = 0; q < C; ++q) {
-                const double f = rescale(cl_ld_f32(&sh.m, q), M, P.log2e_t);
-                s_out += cl_ld_f64(&sh.s_out, q) * f;
-                s_in += cl_ld_f64(&sh.s_in, q) * f;
-                bad |= cl_ld_s32(&sh.bad, q);
-            }
-            sd::cl_sync();                          // nobody leaves, or overwrites logits, while others may still read
-        }
-        S = s_out + s_in;
-        mass_p = block_sum(mass_p, sh.wsum, lane, warp);
-        const double R0 = P.lse ? fmax(0.0, 1.0 - mass_p) : 0.0;
-        const double R = s_out > 0.0 ? R0 : 0.0;    // a draft with nothing outside the list has no such outcome
-        mass = mass_p + R;
-        const double share = R > 0.0 ? R * S / s_out : 0.0;
-        f_out = mass - share;
-        const bool empty = S == 0.0;                // no logit above -inf
-        if (rank == 0) {
-            double pz = 0.0;                        // sum p (z - m): differences first, whatever the logits' size
-            for (int i = tid; i < k; i += THREADS)
-                if (ids[i] >= 0 && prob[i] != 0.0) pz += prob[i] * ((double)zs[i] - (double)reference(M));
-            plogp = block_sum(plogp, sh.wsum, lane, warp);
-            pz = block_sum(pz, sh.wsum, lane, warp);
-            if (tid == 0) {
-                float loss;
-                if (bad) loss = NAN;
-                else if (!any) loss = 0.f;
-                else if (empty) loss = mass_p > 0.0 ? INFINITY : 0.f;
-                else {
-                    double l = plogp;
-                    if (mass_p > 0.0) l += mass_p * log(S) - pz / P.T;
-                    if (R > 0.0) l += R * (log(R) - log(s_out / S));
-                    loss = (float)(S != S ? (double)NAN : l);
-                }
-                P.loss[row_id] = loss;
-                if (bad) atomicOr(P.status, SPECDEC_DATA_BAD_TOKEN);
-                if (MODE == DistillMode::Loss) {
-                    float* sv = P.saved + (size_t)row_id * 4;
-                    sv[0] = reference(M);
-                    sv[1] = (float)S;
-                    sv[2] = (float)f_out;
-                    sv[3] = !any || bad || empty ? -1.f : (float)mass;
-                }
+                s_out += fold2(acc);
+                s_in += in;
+            } else {
+                huge_terms(S, bitmap, j0, top, lane, s_out, s_in);
             }
         }
-        M = reference(M);
-        zero = !any || bad || empty;
-    } else if (MODE == DistillMode::Gradient) {
-        M = saved_m;
-        S = saved_s;
-        f_out = saved_out;
-        mass = saved_mass;
-        __syncthreads();                            // the listed logits are in shared memory: the gradient may lie on the logits
-    } else if (STATS && rank == 0 && tid == 0) {    // Step with weight 0
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            s_out += __shfl_xor_sync(0xffffffffu, s_out, o);
+            s_in += __shfl_xor_sync(0xffffffffu, s_in, o);
+        }
+        // ---- this warp's record.  Differences of logits are formed first, whatever the logits' size
+        double g_sum = 0.0;
+        float z_ref = -INFINITY;
+        if (warp * 32 < k) {
+            for (int i = tid; i < k; i += NT)
+                if (ids[i] >= 0 && prob[i] != 0.0) z_ref = fmaxf(z_ref, zs[i]);
+            z_ref = reference(warp_max(z_ref));
+            for (int i = tid; i < k; i += NT)
+                if (ids[i] >= 0 && prob[i] != 0.0) g_sum += prob[i] * ((double)zs[i] - (double)z_ref);
+            e_sum = warp_sum(e_sum);
+            f_sum = warp_sum(f_sum);
+            g_sum = warp_sum(g_sum);
+            flags = __reduce_or_sync(0xffffffffu, flags);
+        }
+        if (lane == 0) sh.record[warp] = Record{e_sum, f_sum, g_sum, s_out, s_in, top, z_ref, flags};
+        if (C > 1) sd::cl_sync(); else __syncthreads();
+        double plogp = 0.0, pz = 0.0, S_out = 0.0, R = 0.0;
+        if (warp == 0) {
+            // ---- the row's sums, by every CTA for itself; two records a lane
+            Record rec[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int q = h * 32 + lane;
+                rec[h] = Record{0.0, 0.0, 0.0, 0.f, 0.f, -INFINITY, 0.f, 0};
+                if (q < C * NW) {
+                    const Record* from = &sh.record[q % NW];
+                    const uint32_t at = q / NW;
+                    rec[h].s_out = cl_ld_f32(&from->s_out, at);
+                    rec[h].s_in = cl_ld_f32(&from->s_in, at);
+                    rec[h].m = cl_ld_f32(&from->m, at);
+                    if (q % NW * 32 < k) {
+                        rec[h].e = cl_ld_f64(&from->e, at);
+                        rec[h].f = cl_ld_f64(&from->f, at);
+                        rec[h].g = cl_ld_f64(&from->g, at);
+                        rec[h].z_ref = cl_ld_f32(&from->z_ref, at);
+                        rec[h].flags = cl_ld_s32(&from->flags, at);
+                    }
+                }
+            }
+            const float all = warp_max(fmaxf(rec[0].m, rec[1].m));
+            m = reference(all);
+            double out = 0.0, in = 0.0, e = 0.0, f = 0.0, g = 0.0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float to = move_terms(rec[h].m, all, P.c);
+                out += (double)(rec[h].s_out * to);
+                in += (double)(rec[h].s_in * to);
+                e += rec[h].e;
+                f += rec[h].f;
+                g += rec[h].g + (rec[h].e != 0.0 ? rec[h].e * ((double)rec[h].z_ref - (double)m) : 0.0);
+            }
+            const double exact = unround(m, P.c);
+            S_out = warp_sum(out) * exact;
+            s = S_out + warp_sum(in) * exact;
+            e = warp_sum(e);
+            plogp = warp_sum(f);
+            pz = warp_sum(g);
+            flags = __reduce_or_sync(0xffffffffu, rec[0].flags | rec[1].flags);
+            if (!P.lse) {                           // p = e / sum e
+                plogp = e > 0.0 ? plogp / e - log(e) : e;
+                pz = e > 0.0 ? pz / e : e;
+            }
+            const double p = P.lse ? e : e > 0.0 ? 1.0 : e;         // sum p; NaN stays NaN
+            R = P.lse && S_out > 0.0 ? fmax(0.0, 1.0 - p) : 0.0;     // a draft with nothing outside the list has no rest
+            mass = p + R;
+            const double out_factor = mass - (R > 0.0 ? R * s / S_out : 0.0);
+            zero = flags != 2 || s == 0.0;          // a bad list, an empty one, or no logit above -inf
+            if (lane == 0) {
+                sh.m = m;
+                sh.s = s;
+                sh.mass = mass;
+                sh.e = P.lse || e == 0.0 ? 1.0 : e;         // what e is divided by; a list without mass stays one
+                sh.scale = (float)((double)weight / P.T * out_factor / (s / exact));       // of a term against the rounded m*c
+                sh.zero = zero;
+                if (rank == 0) {
+                    float loss;
+                    if (flags & 1) loss = NAN;
+                    else if (flags == 0) loss = 0.f;
+                    else if (s == 0.0) loss = p > 0.0 ? INFINITY : 0.f;
+                    else {
+                        double l = plogp;
+                        if (p > 0.0) l += p * log(s) - pz / P.T;
+                        if (R > 0.0) l += R * (log(R) - log(S_out / s));
+                        loss = s == s ? (float)l : NAN;
+                    }
+                    P.loss[row_id] = loss;
+                    if (flags & 1) atomicOr(P.status, SPECDEC_DATA_BAD_TOKEN);
+                    if (MODE == DistillMode::Loss)
+                        *reinterpret_cast<float4*>(P.saved + (size_t)row_id * 4) = make_float4(m, (float)(s / exact), (float)out_factor, zero ? -1.f : (float)mass);
+                }
+            }
+        }
+        if (C > 1) sd::cl_sync(); else __syncthreads();      // nobody leaves, or writes over logits, while others still read
+        if (!GRAD) return;
+        m = sh.m;
+        s = sh.s;
+        mass = sh.mass;
+        scale = sh.scale;
+        zero = sh.zero;
+        e_sum = sh.e;
+    } else if (STATS && rank == 0 && tid == 0) {    // a step of weight 0
         P.loss[row_id] = 0.f;
     }
-    if constexpr (!GRAD) return;
-
-    // ---- the gradient
-    const double wt = (double)weight / P.T;
-    const float scale = zero ? 0.f : (float)(wt * f_out / S);
-    const f2 hi2 = sd::pack2(P.c.hi, P.c.hi), lo2 = sd::pack2(P.c.lo, P.c.lo), neg = sd::pack2(-M, -M), scale2 = sd::pack2(scale, scale);
-    const int tiles = (v1 - v0 + TILE - 1) / TILE;
-    for (int n = 0; n < tiles; ++n) {               // from the tile that the registers hold: the last one, or the first
-        const int t0 = v0 + (STATS ? tiles - 1 - n : n) * TILE;
-        if (!zero && n > 0) load_tile<T>(row, shift, V, t0, v1, tid, r);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = t0 + i * THREADS + tid;
-            if (j >= v1) continue;
-            float g[N];
-            if (zero) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) g[e] = 0.f;
+    if constexpr (GRAD) {
+        const float u = m * P.c;
+        if (MODE == DistillMode::Gradient && !zero) {
+            s *= unround(m, P.c);                   // against m itself
+            if (!P.lse) {                           // the list's sum
+                e_sum = warp_sum(e_sum);
+                if (lane == 0) sh.record[warp].e = e_sum;
+                __syncthreads();
+                e_sum = 0.0;
+                for (int w = 0; w < NW; ++w) e_sum += sh.record[w].e;
+                if (e_sum == 0.0) e_sum = 1.0;
             } else {
+                e_sum = 1.0;
+            }
+        }
+        // ---- the gradient, from the chunk that the registers hold: the last one, or the first
+        T* grad = static_cast<T*>(P.grad) + row_id * P.g_stride;
+        const bool wide = row_shift(grad) == S.shift;
+        const f2 c2 = sd::pack2(P.c, P.c), neg = sd::pack2(-u, -u), scale2 = sd::pack2(scale, scale);
+        const bool normal = ordinary(m);
+        for (int n = 0; n < own_steps; ++n) {
+            const int j0 = j_first + (STATS ? own_steps - 1 - n : n) * stride;
+            if (!zero && n > 0) {
+                S.fetch(j0, lane, sh.chunk[warp]);
+                chunk_wait();
+#pragma unroll
+                for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int j = j0 + i * 32 + lane;
+                if (i >= S.depth || j >= S.v1) continue;
+                float g[N];
                 f2 x[N / 2];
                 pairs(r[i], x, T());
 #pragma unroll
-                for (int q = 0; q < N / 2; ++q) sd::unpack2(sd::mul2(term2(x[q], neg, hi2, lo2), scale2), g[2 * q], g[2 * q + 1]);
+                for (int q = 0; q < N / 2; ++q) sd::unpack2(sd::mul2(term2(x[q], c2, neg), scale2), g[2 * q], g[2 * q + 1]);
+                if (!normal || zero) {
+                    widen<T>(r[i], g);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) g[e] = zero ? 0.f : huge_term(g[e], m) * scale;
+                }
+                store_vec<T>(grad, S.shift, S.V, j, wide, g);
             }
-            store_vec<T>(grad, shift, V, j, wide, g);
         }
-    }
-    if (zero) return;
-    __syncthreads();                                // the CTA's part is written: the listed tokens are written over
-    for (int i = tid; i < k; i += THREADS) {
-        const int id = ids[i];
-        const int at = (id + shift) / N;
-        if (id < 0 || at < v0 || at >= v1) continue;
-        const double q = exp(((double)zs[i] - (double)M) / P.T) / S;
-        store_one(grad + id, (float)(wt * (mass * q - prob[i])));
+        if (zero) return;
+        __syncthreads();                            // the CTA's part is written: the listed tokens are written over
+        const double wt = (double)weight / P.T;
+        for (int i = tid; i < k; i += NT)
+            if (const int id = ids[i]; id >= 0) {
+                const double q = exp(((double)zs[i] - (double)m) / P.T) / s;
+                store_one(grad + id, (float)(wt * (mass * q - prob[i] / e_sum)));
+            }
     }
 }
 
@@ -336,9 +411,10 @@ cudaError_t launch_as(const DistillParams& p, DistillMode mode, int rows, size_t
 cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mode, int rows, int sm_count, cudaStream_t s) {
     const int n = dtype == SPECDEC_F32 ? 4 : 8;
     const int most = (p.V + 2 * n - 2) / n;        // vectors of a row at its worst alignment
-    p.cluster = rw::cluster_size(rows, (p.V + n - 1) / n, sm_count);
+    const int hold = NW * CHUNK;                   // vectors that a CTA's registers hold
+    p.cluster = rw::cluster_size(rows, most, sm_count, std::min(MAX_CLUSTER, (most + hold - 1) / hold));
     p.slice_words = ((most + p.cluster - 1) / p.cluster * n + 31) / 32;
-    const size_t smem = (size_t)p.slice_words * 4 + (size_t)p.k * 16;
+    const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 16;
     if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, smem, s);
     if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, smem, s);
     return launch_as<__half>(p, mode, rows, smem, s);

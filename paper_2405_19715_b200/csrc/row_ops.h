@@ -5,14 +5,7 @@
 
 namespace rw {
 
-// log2(e)/T in two floats: its rounding to one would put the same relative error of 6e-8 * |x - m| into every term of
-// a sum.  hi is rounded down, so that lo is positive and a term of -inf stays 2^-inf.
-struct Scale {
-    float hi, lo;
-};
-
-// Sum of 2^((x - m) * log2(e)/T) over a part of a row, m the part's largest value (-inf: nothing above it, s is then
-// a sum against 0).
+// Sum of exp((x - m) / T) over a part of a row, m the part's largest value; against 0 if that is -inf.
 struct Part {
     double s;
     float m;
@@ -23,8 +16,8 @@ struct Part {
 struct TopParams {
     const void* x;
     long long outer_stride, row_stride;       // elements; row i is outer i / inner, row i % inner
-    int inner, V, k, cluster;
-    rw::Scale c;
+    int rows, inner, V, k, cluster;
+    float c;                                  // log2(e) / T
     double T, log2e_t;
     float* values;                            // [rows, k]
     int32_t* tokens;                          // [rows, k]
@@ -42,7 +35,6 @@ struct BeamParams {
     const float* scores;                      // [B * W]
     const int32_t* finished;                  // [B * W] or null
     int W, V, k, M, end_token;
-    rw::Scale c;
     double T;
     float* out_scores;                        // [B, M]
     int32_t* out_parents;
@@ -70,7 +62,7 @@ struct DistillParams {
     const int32_t* tokens;
     const float* lse;                         // null: renormalised over the list
     int V, k, cluster, slice_words;
-    rw::Scale c;
+    float c;                                  // log2(e) / T
     double T, log2e_t;
     float* loss;
     float* saved;                             // [rows, 4]: written by the loss alone, read by the gradient alone

@@ -12,9 +12,8 @@ namespace rw {
 
 using sd::f2;
 
-constexpr int THREADS = 512, WARPS = THREADS / 32;
+constexpr int NT = 256, NW = NT / 32;          // threads of a CTA
 constexpr int NV = 8;                          // 16-byte vectors a thread holds: 32 registers
-constexpr int TILE = THREADS * NV;             // vectors of a row that a CTA holds at a time (64 KB)
 constexpr int MAX_CLUSTER = 8;
 
 template <typename T> struct Row;
@@ -23,18 +22,21 @@ template <> struct Row<float> {
     static __device__ __forceinline__ float wide(float v) { return v; }
     static __device__ __forceinline__ uint32_t bits(float v) { return __float_as_uint(v); }
     static __device__ __forceinline__ uint32_t neg_inf() { return 0xff800000u; }
+    static __device__ __forceinline__ float lowest() { return -INFINITY; }
 };
 template <> struct Row<__nv_bfloat16> {
     static constexpr int N = 8, KEY_BITS = 16;
     static __device__ __forceinline__ float wide(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ uint32_t bits(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
     static __device__ __forceinline__ uint32_t neg_inf() { return 0xff80ff80u; }
+    static __device__ __forceinline__ __nv_bfloat16 lowest() { return __ushort_as_bfloat16(0xff80u); }
 };
 template <> struct Row<__half> {
     static constexpr int N = 8, KEY_BITS = 19;   // fp16 widened to fp32: sign, 8 exponent bits, 10 of the mantissa
     static __device__ __forceinline__ float wide(__half v) { return __half2float(v); }
     static __device__ __forceinline__ uint32_t bits(__half v) { return __half_as_ushort(v); }
     static __device__ __forceinline__ uint32_t neg_inf() { return 0xfc00fc00u; }
+    static __device__ __forceinline__ __half lowest() { return __ushort_as_half(0xfc00u); }
 };
 
 // The elements of a vector as fp32, two to a packed register pair; widening is exact.
@@ -55,30 +57,56 @@ __device__ __forceinline__ void widen(const uint4& r, float (&x)[Row<T>::N]) {
     for (int q = 0; q < Row<T>::N / 2; ++q) sd::unpack2(p[q], x[2 * q], x[2 * q + 1]);
 }
 
-// Largest element of a vector; NaN if it holds one.
+// Largest element of a vector, NaN if it holds one; the 16-bit types keep two candidates side by side until the value is
+// asked for.  Reach says whether such a maximum is not below a bound (NaN is not), which the 16-bit types round up to the
+// next value that they have.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-__device__ __forceinline__ float vec_max(const uint4& r, float) {
-    return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
-}
-__device__ __forceinline__ float vec_max(const uint4& r, __nv_bfloat16) {
-    uint32_t a, b, m;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(r.x), "r"(r.y));
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(r.z), "r"(r.w));
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
-    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-}
-__device__ __forceinline__ float vec_max(const uint4& r, __half) {
-    uint32_t a, b, m;
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(r.x), "r"(r.y));
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(b) : "r"(r.z), "r"(r.w));
-    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&m));
-    return max_nan(v.x, v.y);
-}
+template <typename P> __device__ __forceinline__ P as_pair(uint32_t w) { return *reinterpret_cast<const P*>(&w); }
+template <typename T> struct Max;
+template <> struct Max<float> {
+    float v;
+    __device__ __forceinline__ explicit Max(const uint4& r) {
+        v = max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+    }
+    __device__ __forceinline__ Max(const Max& a, const Max& b) { v = max_nan(a.v, b.v); }
+    __device__ __forceinline__ float value() const { return v; }
+};
+template <> struct Max<__nv_bfloat16> {
+    __nv_bfloat162 v;
+    __device__ __forceinline__ explicit Max(const uint4& r) {
+        v = __hmax2_nan(__hmax2_nan(as_pair<__nv_bfloat162>(r.x), as_pair<__nv_bfloat162>(r.y)), __hmax2_nan(as_pair<__nv_bfloat162>(r.z), as_pair<__nv_bfloat162>(r.w)));
+    }
+    __device__ __forceinline__ Max(const Max& a, const Max& b) { v = __hmax2_nan(a.v, b.v); }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(v), __high2float(v)); }
+};
+template <> struct Max<__half> {
+    __half2 v;
+    __device__ __forceinline__ explicit Max(const uint4& r) {
+        v = __hmax2_nan(__hmax2_nan(as_pair<__half2>(r.x), as_pair<__half2>(r.y)), __hmax2_nan(as_pair<__half2>(r.z), as_pair<__half2>(r.w)));
+    }
+    __device__ __forceinline__ Max(const Max& a, const Max& b) { v = __hmax2_nan(a.v, b.v); }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(v), __high2float(v)); }
+};
+template <typename T> struct Reach;
+template <> struct Reach<float> {
+    float b;
+    __device__ __forceinline__ explicit Reach(float x) { b = x; }
+    __device__ __forceinline__ bool operator()(const Max<float>& m) const { return !(m.v < b); }
+};
+template <> struct Reach<__nv_bfloat16> {
+    __nv_bfloat162 b;
+    __device__ __forceinline__ explicit Reach(float x) { b = __bfloat162bfloat162(__float2bfloat16_ru(x)); }
+    __device__ __forceinline__ bool operator()(const Max<__nv_bfloat16>& m) const { return __hgeu2_mask(m.v, b) != 0u; }
+};
+template <> struct Reach<__half> {
+    __half2 b;
+    __device__ __forceinline__ explicit Reach(float x) { b = __half2half2(__float2half_ru(x)); }
+    __device__ __forceinline__ bool operator()(const Max<__half>& m) const { return __hgeu2_mask(m.v, b) != 0u; }
+};
 
 // Keys: larger value <-> larger key, NaN below everything, -0 and +0 alike; with the token in the low word a
 // larger key also means the lower of two tokens that tie.
@@ -104,69 +132,89 @@ template <typename T>
 __device__ __forceinline__ int row_vectors(int shift, int V) { return (shift + V + Row<T>::N - 1) / Row<T>::N; }
 
 template <typename T>
-__device__ __noinline__ uint4 load_edge(const T* row, int e0, int V) {
+__device__ __forceinline__ uint4 edge_vector(const T* row, int e0, int V) {
     constexpr int N = Row<T>::N, PER = 4 / sizeof(T);
-    uint32_t w[4];
+    uint32_t b[N], w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        w[q] = Row<T>::neg_inf();
+    for (int e = 0; e < N; ++e) b[e] = e0 + e >= 0 && e0 + e < V ? Row<T>::bits(__ldcg(row + e0 + e)) : Row<T>::neg_inf() & (PER == 1 ? 0xffffffffu : 0xffffu);
 #pragma unroll
-        for (int h = 0; h < PER; ++h) {
-            const int e = e0 + q * PER + h;
-            if (e >= 0 && e < V) {
-                const uint32_t b = Row<T>::bits(row[e]);
-                if constexpr (PER == 1) w[q] = b;
-                else w[q] = h ? ((w[q] & 0xffffu) | (b << 16)) : ((w[q] & 0xffff0000u) | b);
+    for (int q = 0; q < 4; ++q) w[q] = PER == 1 ? b[q] : b[q * PER] | (b[q * PER + PER - 1] << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A CTA's part of a row, [v0, v1) of its vectors, in chunks that a warp holds at a time: 32 * depth vectors, 8 of them a
+// lane (4 KB) unless the part is too short to give every warp such a chunk.  Every warp has a range of chunks that follow
+// one another.  Vectors [in0, in0 + in_n) lie inside the row.
+constexpr int CHUNK = 32 * NV;
+template <typename T>
+struct Slice {
+    const T* row;
+    int shift, V, v0, v1, in0, in_n, depth, base, extra;
+    __device__ __forceinline__ Slice(const T* row_, int V_, int C, int rank) {
+        row = row_;
+        V = V_;
+        shift = row_shift(row);
+        const int nvec = row_vectors<T>(shift, V), per = C > 1 ? (nvec + C - 1) / C : nvec;
+        v0 = min(nvec, rank * per);
+        v1 = min(nvec, v0 + per);
+        in0 = max(v0, shift ? 1 : 0);
+        in_n = max(0, min(v1, (shift + V) / Row<T>::N) - in0);
+        depth = min(NV, max(1, (v1 - v0 + NT - 1) / NT));
+        const int chunks = (v1 - v0 + 32 * depth - 1) / (32 * depth);
+        base = chunks / NW;                        // every warp has that many, the first `extra` one more
+        extra = chunks % NW;
+    }
+    __device__ __forceinline__ int first_chunk(int warp) const { return warp * base + min(warp, extra); }
+    __device__ __forceinline__ int chunks_of(int warp) const { return base + (warp < extra ? 1 : 0); }
+    __device__ __forceinline__ int steps() const { return base + (extra ? 1 : 0); }      // of the warp that has most
+    __device__ __forceinline__ int start(int chunk) const { return v0 + chunk * 32 * depth; }
+    __device__ __forceinline__ bool inside(int j) const { return (unsigned)(j - in0) < (unsigned)in_n; }
+    __device__ __forceinline__ const T* address(int j) const { return row + ((long long)j * Row<T>::N - shift); }
+    // The copy into shared memory of the chunk that starts at vector j0, asynchronous: it costs no register while it is on
+    // its way.  A lane reads back, after chunk_wait(), only what it has asked for itself: vector j0 + i * 32 + lane at
+    // buffer[i * 32 + lane].  -inf where there is no vector.
+    __device__ __forceinline__ void fetch(int j0, int lane, uint4* buffer) const {
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(buffer + lane);
+        if (depth == NV && j0 >= in0 && j0 + CHUNK <= in0 + in_n) {
+            const T* p = address(j0 + lane);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(p + i * 32 * Row<T>::N) : "memory");
+        } else {
+            const uint32_t w = Row<T>::neg_inf();
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i) {
+                const int j = i < depth ? j0 + i * 32 + lane : v1;
+                if (inside(j)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(address(j)) : "memory");
+                else buffer[i * 32 + lane] = j < v1 ? edge_vector<T>(row, j * Row<T>::N - shift, V) : make_uint4(w, w, w, w);
             }
         }
     }
-    (void)N;
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-template <typename T>
-__device__ __forceinline__ uint4 load_vec(const T* row, int shift, int V, int j) {
-    constexpr int N = Row<T>::N;
-    const int e0 = j * N - shift;
-    if (e0 >= 0 && e0 + N <= V) return __ldcg(reinterpret_cast<const uint4*>(row + e0));
-    return load_edge<T>(row, e0, V);
-}
-// This thread's share of tile t0: vectors t0 + i*THREADS + tid below v1; -inf where there is none.
-template <typename T>
-__device__ __forceinline__ void load_tile(const T* row, int shift, int V, int t0, int v1, int tid, uint4 (&r)[NV]) {
-    const uint32_t w = Row<T>::neg_inf();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int j = t0 + i * THREADS + tid;
-        r[i] = j < v1 ? load_vec<T>(row, shift, V, j) : make_uint4(w, w, w, w);
-    }
-}
+};
+__device__ __forceinline__ void chunk_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// 2^((x - m) * log2(e)/T).  x - m is formed before scaling: rows masked with the type's lowest value neither overflow
-// nor turn into NaN.
-__device__ __forceinline__ f2 term2(f2 x, f2 neg_m, f2 hi, f2 lo) {
-    const f2 d = sd::add2(x, neg_m);
-    return sd::ex2_2(sd::fma2(d, lo, sd::mul2(d, hi)));
-}
+// Softmax terms 2^(x*c - u), c = log2(e)/T, u a reference in the same unit.  u is kept as it was rounded, and c's own
+// rounding to 32 bits (2^-25) scales distances to the reference alone, so one multiply-add per term loses nothing.
+__device__ __forceinline__ f2 term2(f2 x, f2 c, f2 neg_u) { return sd::ex2_2(sd::fma2(x, c, neg_u)); }
 // Sum of a vector's terms; fp32 is enough for the eight terms of a vector and the eight vectors of a thread, the
 // sums of threads are added in 64 bits.
 template <int NP>
-__device__ __forceinline__ f2 terms(const f2 (&x)[NP], f2 neg_m, f2 hi, f2 lo) {
+__device__ __forceinline__ f2 terms(const f2 (&x)[NP], f2 c, f2 neg_u) {
     if constexpr (NP == 4)
-        return sd::add2(sd::add2(term2(x[0], neg_m, hi, lo), term2(x[1], neg_m, hi, lo)),
-                        sd::add2(term2(x[2], neg_m, hi, lo), term2(x[3], neg_m, hi, lo)));
+        return sd::add2(sd::add2(term2(x[0], c, neg_u), term2(x[1], c, neg_u)), sd::add2(term2(x[2], c, neg_u), term2(x[3], c, neg_u)));
     else
-        return sd::add2(term2(x[0], neg_m, hi, lo), term2(x[1], neg_m, hi, lo));
+        return sd::add2(term2(x[0], c, neg_u), term2(x[1], c, neg_u));
 }
 __device__ __forceinline__ float fold2(f2 a) {
     float x, y;
     sd::unpack2(a, x, y);
     return x + y;
 }
-__device__ __forceinline__ float term(float x, float m, Scale c) {
-    const float d = x - m;
-    return sd::ex2(fmaf(d, c.lo, d * c.hi));
-}
-
+// Logits so large that x*c could overflow (rows masked with the type's lowest value) do not go through a multiply-add:
+// there two values are equal or too far apart for the smaller one to count.
+constexpr float HUGE_LOGIT = 1.0e30f;
+__device__ __forceinline__ bool ordinary(float m) { return m <= HUGE_LOGIT && m >= -HUGE_LOGIT; }
+__device__ __forceinline__ float huge_term(float x, float m) { return x == m ? 1.f : x == x ? 0.f : x; }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -176,6 +224,12 @@ __device__ __forceinline__ double warp_sum(double v) {
 __device__ __forceinline__ double rescale(float from, float to, double c) {   // factor that moves a sum to another reference
     return from == to ? 1.0 : exp2(((double)from - (double)to) * c);
 }
+// The same for a thread's sum of terms, whose references are m*c as rounded to 32 bits; 0 from -inf, where the sum is 0.
+__device__ __forceinline__ float move_terms(float from, float to, float c) {
+    return from == to ? 1.f : ordinary(from) && ordinary(to) ? sd::ex2(from * c - to * c) : 0.f;
+}
+// The factor from sums against the rounded m*c to sums against m itself.
+__device__ __forceinline__ double unround(float m, float c) { return ordinary(m) ? exp2((double)(m * c) - (double)m * (double)c) : 1.0; }
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
 __device__ __forceinline__ double cl_ld_f64(const double* p, uint32_t rank) { return sd::cl_ld_f64(sd::cl_map(p, rank)); }
@@ -190,24 +244,23 @@ __device__ __forceinline__ unsigned long long cl_ld_u64(const unsigned long long
 // Largest of the non-NaN lane values.
 __device__ __forceinline__ float warp_max(float v) { return sd::warp_max(v); }
 
-// CTAs per row.  A row that does not fit one CTA's registers is spread over a cluster; with few rows more CTAs
-// share a row, down to 2 KB each, as long as every one of them can have an SM of its own.
-inline int cluster_size(long long rows, int nvec, int sm_count) {
-    int C = 1;
-    while (C < MAX_CLUSTER && C * TILE < nvec) C *= 2;
-    while (C < MAX_CLUSTER && rows * C * 2 <= sm_count && nvec >= 256 * C) C *= 2;
+// CTAs per row beyond `least`: with few rows more of them share a row, down to 2 KB each, as long as every one can have
+// an SM of its own.
+inline int cluster_size(long long rows, int nvec, int sm_count, int least) {
+    int C = least;
+    while (2 * C <= MAX_CLUSTER && rows * C * 2 <= sm_count && nvec >= 256 * C) C *= 2;
     return C;
 }
 
 template <typename P>
-inline cudaError_t launch(void (*kernel)(P), const P& p, long long rows, int C, size_t smem, cudaStream_t s) {
+inline cudaError_t launch(void (*kernel)(P), const P& p, long long clusters, int C, size_t smem, cudaStream_t s) {
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * C));
-    cfg.blockDim = dim3(THREADS);
+    cfg.gridDim = dim3((unsigned)(clusters * C));
+    cfg.blockDim = dim3(NT);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute a[1];

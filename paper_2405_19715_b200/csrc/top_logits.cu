@@ -1,293 +1,535 @@
 // The k largest logits of a row in order, and the row's log-sum-exp: what a draft model's training keeps of a target
 // row, and what beam selection starts from.
 //
-// The row passes through registers once.  A CTA holds a tile of 4096 16-byte vectors (8 per thread); rows of more
-// are spread over a thread-block cluster, longer ones still walked tile by tile.  Per tile:
-//   1. thread maxima; per warp the r-th largest of them, r = ceil(k / 16): the least of these over the 16 warps is a
-//      lower bound on the tile's k-th largest (k threads hold an element at or above it), and a close one because
-//      few of the k largest share a thread;
-//   2. the softmax terms are summed against the tile's maximum, and the elements at or above the bound, k and some
-//      tens, go into a buffer in shared memory;
-//   3. each of them finds its rank by counting the larger ones.  Keys carry the token, so no two are equal, ranks
-//      are unique and the result does not depend on the order of arrival.
-// Where the bound lets too many through (masked rows, ties, values that grow along the row), the k-th largest value
-// is found by counting over the registers, and ties with it are taken in token order.
-// The CTAs of a cluster then read one another's lists and each places its own entries.
+// The row passes through registers once.  The 8 warps of a CTA have a stretch of it each, and go through it by themselves
+// in chunks of 4 KB, the next one on its way into shared memory meanwhile.
+//   The bound.  The r-th largest of the 256 thread maxima of the warps' first chunks, which are a sample of the row, with
+//     r the number of the k largest that such a sample should hold and 2.5 standard deviations more: about k and half as
+//     many of the row's elements reach it.
+//   Every warp keeps the vectors that reach the bound.  At the end their elements that reach it join a buffer, and each
+//     finds its rank by counting the larger ones.  Keys carry the token, so no two are equal, ranks are unique and the
+//     result does not depend on the order of arrival.
+//   Where fewer than k elements reach the bound, or more vectors than a warp can keep (the sample has missed the row's
+//     large logits, masked rows, ties), careful_pass reads the row once more, and takes the bound from the k largest that
+//     it has seen so far.
+// Softmax terms are summed by each warp against the largest value that it has met; the sums meet at the end, in 64 bits.
+// With few rows a row is cut over the CTAs of a cluster, which then read one another's lists, and each places its own
+// entries.
 #include "rows.cuh"
 
 namespace {
 
 using namespace rw;
 
-constexpr int CAP = 2048;                  // candidates in shared memory: MAX_CLUSTER lists of MAX_TOP entries, too
 constexpr int MAX_TOP = SPECDEC_TOP_LOGITS_MAX;
-static_assert(CAP >= MAX_CLUSTER * MAX_TOP && MAX_TOP <= THREADS, "the lists of a cluster fit the buffer");
+constexpr int CAP = 2048;                  // elements in the buffer
+constexpr int KEEP = 96;                   // vectors a warp can keep
+constexpr int PER_SM = 3;                  // CTAs of an SM; a fourth would leave 64 registers, and measured 10 % slower
+static_assert(MAX_TOP <= NT && CAP >= 2 * MAX_TOP && CAP % NT == 0, "the lists fit the buffer");
+static_assert(MAX_CLUSTER * MAX_TOP * 8 <= NW * CHUNK * 16, "the lists of a cluster fit the chunks");
 
+// Everything that all threads share lives here, the row's geometry among it: the registers of a thread hold its vectors.
+template <typename T>
 struct TopShared {
+    Slice<T> S;
+    uint4 chunk[NW][CHUNK];                // each warp's coming chunk; at the end the lists of the cluster
+    union {
+        uint4 vec[NW][KEEP];
+        int place[CAP];                    // of the buffer's entries, while they are ranked
+    };
+    int vec_at[NW][KEEP];                  // which vector of the row it is
     unsigned long long buf[CAP];
-    unsigned long long list[2][MAX_TOP];
-    double wsum[WARPS];
-    float wmax[WARPS], wrth[WARPS];
-    int wcount[2][WARPS];
-    int count, n_list;
+    unsigned long long list[MAX_TOP];
+    double wsum[NW];
+    float tmax[NT], wmax[NW];
+    int wcount[2][NW];
+    int count, n_list;                     // elements in the buffer (or that would be), length of the list
+    float first_bound;
     Part part;
 };
 
-// r-th largest of the lane values; -inf when fewer than r are above -inf.
-__device__ __forceinline__ float warp_rth_largest(float v, int r, int lane) {
-    float cur = -INFINITY;
-    for (int it = 0; it < r; ++it) {
-        cur = warp_max(v);
-        if (cur == -INFINITY) break;
-        const unsigned who = __ballot_sync(0xffffffffu, v == cur);
-        if (lane == __ffs(who) - 1) v = -INFINITY;
+// The r-th largest of the 256 thread maxima, or a value just below it (its key's leading 16 bits); -inf if fewer are
+// above -inf.  One warp; r <= NT.
+__device__ __forceinline__ float rth_of_maxima(const float (&tmax)[NT], int r, int lane) {
+    uint32_t key[NT / 32];
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) key[i] = value_key(tmax[i * 32 + lane]) >> 16;
+    uint32_t least = key[0], most = key[0];
+#pragma unroll
+    for (int i = 1; i < NT / 32; ++i) { least = min(least, key[i]); most = max(most, key[i]); }
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    const int bits = 32 - __clz(least ^ most);       // the leading bits are those of all of them
+    uint32_t prefix = most >> bits << bits;
+#pragma unroll 1
+    for (int bit = bits - 1; bit >= 0; --bit) {
+        const uint32_t trial = prefix | (1u << bit);
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 32; ++i) c += key[i] >= trial ? 1 : 0;
+        if ((int)__reduce_add_sync(0xffffffffu, c) >= r) prefix = trial;
     }
-    return cur;
+    return prefix > 0x007f ? key_value(prefix << 16) : -INFINITY;
 }
 
 // Sum of one int per thread over the CTA; `buf` alternates between two sets so that one barrier is enough.
-__device__ __forceinline__ int block_count(int v, int (&slot)[WARPS], int lane, int warp) {
+__device__ __forceinline__ int block_count(int v, int (&slot)[NW], int lane, int warp) {
     v = __reduce_add_sync(0xffffffffu, v);
     if (lane == 0) slot[warp] = v;
     __syncthreads();
     int n = 0;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) n += slot[w];
+    for (int w = 0; w < NW; ++w) n += slot[w];
     return n;
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ int count_if(const uint4 (&r)[NV], F f) {
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float x[Row<T>::N];
-        widen<T>(r[i], x);
-#pragma unroll
-        for (int e = 0; e < Row<T>::N; ++e) n += f(x[e]) ? 1 : 0;
-    }
-    return n;
-}
-
-// The `need` largest of the tile (it has that many elements), appended to the buffer.  By counting: the value of the
-// need-th largest is built from its key's leading bits, elements above it are all taken, those equal to it in token
-// order.  Called by the whole CTA, rarely.
+// The buffer's n entries, ranked: the best k of them, in order, into the list, and back to the front of the buffer.
+// Called by the whole CTA; the buffer is complete.
 template <typename T>
-__device__ __noinline__ void exact_select(const uint4 (&r)[NV], int shift, int V, int t0, int v1, int need, TopShared& sh, int tid) {
-    constexpr int N = Row<T>::N;
+__device__ __noinline__ void rank_buffer(TopShared<T>& sh, int n, int k, int tid) {
     const int lane = tid & 31, warp = tid >> 5;
+    if (n > 2 * MAX_TOP) {
+        // many entries: those below the k-th value, or below a value just under it, are dropped before ranking
+        unsigned long long mine[CAP / NT];
+        uint32_t prefix = 0;
+        int turn = 0;
+#pragma unroll
+        for (int i = 0; i < CAP / NT; ++i) mine[i] = i * NT + tid < n ? sh.buf[i * NT + tid] : 0ull;
+#pragma unroll 1
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t trial = prefix | (1u << bit);
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < CAP / NT; ++i) c += (uint32_t)(mine[i] >> 32) >= trial ? 1 : 0;      // never an absent one
+            c = block_count(c, sh.wcount[turn ^= 1], lane, warp);
+            if (c >= k) {
+                prefix = trial;
+                if (c <= k + k / 8 + 16) break;
+            }
+        }
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CAP / NT; ++i)
+            if (i * NT + tid < n && (uint32_t)(mine[i] >> 32) >= prefix) sh.buf[atomicAdd(&sh.count, 1)] = mine[i];
+        __syncthreads();
+        n = sh.count;
+    }
+    // every warp counts over an eighth of the entries, for all of them, four to a lane at a time
+    for (int i = tid; i < n; i += NT) sh.place[i] = 0;
+    __syncthreads();
+    const int q0 = warp * n / NW, q1 = (warp + 1) * n / NW;
+    for (int i0 = 0; i0 < n; i0 += 128) {
+        unsigned long long key[4];
+        int place[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            key[e] = i0 + e * 32 + lane < n ? sh.buf[i0 + e * 32 + lane] : ~0ull;
+            place[e] = 0;
+        }
+#pragma unroll 2
+        for (int q = q0; q < q1; ++q) {
+            const unsigned long long x = sh.buf[q];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) place[e] += x > key[e] ? 1 : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (place[e]) atomicAdd(&sh.place[i0 + e * 32 + lane], place[e]);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += NT)
+        if (sh.place[i] < k) sh.list[sh.place[i]] = sh.buf[i];
+    __syncthreads();
+    const int n_list = min(k, n);
+    if (tid < n_list) sh.buf[tid] = sh.list[tid];
+    if (tid == 0) sh.count = sh.n_list = n_list;
+    __syncthreads();
+}
+
+// Appends the keys of the lanes that have one to the buffer; what does not fit is only counted.  Called by whole warps.
+template <typename T>
+__device__ __forceinline__ void append(TopShared<T>& sh, bool has, unsigned long long key, int lane) {
+    const unsigned who = __ballot_sync(0xffffffffu, has);
+    if (who == 0u) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.count, __popc(who));
+    at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+    if (has && at < CAP) sh.buf[at] = key;
+}
+
+// The k largest of the warps' chunks of one step (all, if there are fewer), appended to the buffer.  By counting over
+// the chunks in shared memory: the value of the k-th largest is built from its key's leading bits; elements above it are
+// all taken, those equal to it in token order.
+template <typename T>
+__device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has, int k, int tid) {
+    constexpr int N = Row<T>::N;
+    const Slice<T>& S = sh.S;
+    const int lane = tid & 31, warp = tid >> 5;
+    const T* mine = reinterpret_cast<const T*>(sh.chunk[warp] + lane);       // element e of vector i: mine[i * 32 * N + e]
+    const int j0 = S.start(chunk) + lane;
+    auto value = [&](int i, int e) { return Row<T>::wide(mine[i * 32 * N + e]); };
+    auto token = [&](int i, int e) { return (j0 + i * 32) * N - S.shift + e; };
+    auto is_real = [&](int i, int e) {
+        const int v = token(i, e);
+        return has && i < S.depth && j0 + i * 32 < S.v1 && v >= 0 && v < S.V;
+    };
     int turn = 0;
-    // level: lo <= x < hi are the elements equal to the need-th largest, hi <= x those above it; `nans`: the level
-    // is NaN, which ranks below everything
+    // elements that are not below f; what lies past the row's ends is -inf
+    auto count_from = [&](float f) {
+        int n = 0;
+#pragma unroll 1
+        for (int i = 0; i < NV; ++i)
+            for (int e = 0; e < N; ++e) n += has && value(i, e) >= f ? 1 : 0;
+        return block_count(n, sh.wcount[turn ^= 1], lane, warp);
+    };
+    // level: lo <= x < hi are the elements equal to the k-th largest, hi <= x those above it; `nans`: the level is NaN,
+    // which ranks below everything
     float lo = -INFINITY, hi = -3.402823466e38f;
     bool nans = false;
-    int above = block_count(count_if<T>(r, [&](float x) { return x >= hi; }), sh.wcount[turn ^= 1], lane, warp);
+    int above = count_from(hi), need = k;
     if (above >= need) {
         uint32_t prefix = 0;
+#pragma unroll 1
         for (int bit = 31; bit >= 32 - Row<T>::KEY_BITS; --bit) {
             const uint32_t trial = prefix | (1u << bit);
-            const float f = key_value(trial);        // a NaN where the trial lies beyond +inf: nothing is counted
-            if (block_count(count_if<T>(r, [&](float x) { return x >= f; }), sh.wcount[turn ^= 1], lane, warp) >= need) prefix = trial;
+            if (count_from(key_value(trial)) >= need) prefix = trial;       // a NaN, beyond +inf: nothing is counted
         }
         lo = key_value(prefix);
         hi = key_value(prefix + (1u << (32 - Row<T>::KEY_BITS)));
-        above = block_count(count_if<T>(r, [&](float x) { return x >= hi; }), sh.wcount[turn ^= 1], lane, warp);
+        above = count_from(hi);
     } else {
-        // fewer than `need` above -inf: the elements past the row's ends, held as -inf, must not count
-        int real = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = t0 + i * THREADS + tid;
-            float x[N];
-            widen<T>(r[i], x);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int v = j * N - shift + e;
-                real += (x[e] == -INFINITY && j < v1 && v >= 0 && v < V) ? 1 : 0;
-            }
-        }
-        const int with_inf = above + block_count(real, sh.wcount[turn ^= 1], lane, warp);
+        int with_inf = 0, real = 0;
+#pragma unroll 1
+        for (int i = 0; i < NV; ++i)
+            for (int e = 0; e < N; ++e)
+                if (is_real(i, e)) {
+                    ++real;
+                    with_inf += value(i, e) >= lo ? 1 : 0;
+                }
+        with_inf = block_count(with_inf, sh.wcount[turn ^= 1], lane, warp);
+        real = block_count(real, sh.wcount[turn ^= 1], lane, warp);
+        need = min(need, real);
         if (with_inf < need) {
             nans = true;
             above = with_inf;
         }
     }
-    int taken = above;                               // ties still wanted: need - taken
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int j = t0 + i * THREADS + tid;
-        float x[N];
-        widen<T>(r[i], x);
-        unsigned ties = 0;
-#pragma unroll
+    // above the level (2), on it (1)?
+    auto where = [&](int i, int e) {
+        if (!is_real(i, e)) return 0;
+        const float x = value(i, e);
+        return nans ? (x == x ? 2 : 1) : x >= hi ? 2 : x >= lo ? 1 : 0;
+    };
+    int ties = 0;
+#pragma unroll 1
+    for (int i = 0; i < NV; ++i)
+        for (int e = 0; e < N; ++e) ties += where(i, e) == 1 ? 1 : 0;
+    block_count(ties, sh.wcount[turn ^= 1], lane, warp);
+    int taken = above;                               // and the ties of the warps before: their tokens are lower
+    for (int w = 0; w < warp; ++w) taken += sh.wcount[turn][w];
+#pragma unroll 1
+    for (int i = 0; i < NV; ++i) {                   // within a warp tokens grow with i, then with the lane, then with e
+        unsigned on = 0;
         for (int e = 0; e < N; ++e) {
-            const int v = j * N - shift + e;
-            const bool real = j < v1 && v >= 0 && v < V;
-            const bool gt = nans ? x[e] == x[e] : x[e] >= hi;
-            const bool eq = nans ? x[e] != x[e] : x[e] >= lo && !(x[e] >= hi);
-            if (real && gt) sh.buf[atomicAdd(&sh.count, 1)] = full_key(x[e], v);
-            if (real && eq) ties |= 1u << e;
+            const int w = where(i, e);
+            append(sh, w == 2, full_key(value(i, e), token(i, e)), lane);
+            if (w == 1) on |= 1u << e;
         }
-        // ties of vectors before this thread's: tokens grow with i, then with the thread, then with e
-        const int mine = __popc(ties);
-        int incl = mine;
+        const int own = __popc(on);
+        int incl = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int t = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += t;
         }
-        int* slot = sh.wcount[turn ^= 1];
-        if (lane == 31) slot[warp] = incl;
-        __syncthreads();
-        int before = incl - mine, all = 0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) before += slot[w];
-            all += slot[w];
+        int before = taken + incl - own;
+        for (int e = 0; e < N; ++e) {
+            const bool tie = (on >> e) & 1u;
+            append(sh, tie && before < need, full_key(value(i, e), token(i, e)), lane);
+            before += tie ? 1 : 0;
         }
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if ((ties >> e) & 1u) {
-                if (taken + before < need) sh.buf[atomicAdd(&sh.count, 1)] = full_key(x[e], j * N - shift + e);
-                ++before;
-            }
-        taken = min(need, taken + all);
+        taken += __shfl_sync(0xffffffffu, incl, 31);
     }
 }
 
+// The list of the k largest (of all, if there are fewer) for rows that the first pass was not made for.  Step by step,
+// a chunk of every warp at a time: elements that exceed the k-th largest so far join the buffer, which is then ranked; a
+// step that has more of them than the buffer holds is counted over.  Called by the whole CTA; nothing is unrolled.
 template <typename T>
-__global__ void __launch_bounds__(THREADS, 2) top_logits_kernel(const __grid_constant__ TopParams P) {
+__device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
     constexpr int N = Row<T>::N;
-    __shared__ TopShared sh;
-    const int C = P.cluster, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int row_id = blockIdx.x / C;
-    const uint32_t rank = blockIdx.x - row_id * C;
-    const int outer = row_id / P.inner, in = row_id - outer * P.inner;
+    const Slice<T>& S = sh.S;
+    const int lane = tid & 31, warp = tid >> 5, steps = S.steps();
+    __syncthreads();
+    if (tid == 0) sh.count = sh.n_list = 0;
+    __syncthreads();
+    // y has to exceed this value, or in a tie with it come before this token; NaN, which ranks last, is let through
+    float least = -INFINITY;
+    int least_token = 0x7fffffff;
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+        const int chunk = S.first_chunk(warp) + step, j0 = S.start(chunk);
+        const bool has = step < S.chunks_of(warp);
+        chunk_wait();
+        if (has) S.fetch(j0, lane, sh.chunk[warp]);
+        chunk_wait();
+        const T* mine = reinterpret_cast<const T*>(sh.chunk[warp] + lane);
+#pragma unroll 1
+        for (int q = 0; q < NV * N; ++q) {
+            const int i = q / N, e = q % N, j = j0 + i * 32 + lane, v = j * N - S.shift + e;
+            const float x = Row<T>::wide(mine[i * 32 * N + e]);
+            append(sh, has && i < S.depth && j < S.v1 && v >= 0 && v < S.V && !(x < least || (x == least && v >= least_token)), full_key(x, v), lane);
+        }
+        __syncthreads();
+        int n = sh.count;
+        __syncthreads();
+        if (n > CAP) {
+            if (tid == 0) sh.count = sh.n_list;     // the list is at the front of the buffer: nothing else was in it
+            __syncthreads();
+            count_over(sh, chunk, has, k, tid);
+            __syncthreads();
+            n = sh.count;
+            __syncthreads();
+        }
+        if (n > sh.n_list) rank_buffer(sh, n, k, tid);
+        if (sh.n_list == k) {
+            const unsigned long long last = sh.list[k - 1];
+            if (last >> 32) {
+                least = key_value((uint32_t)(last >> 32));
+                least_token = key_token(last);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// This thread's terms of a chunk against a value so large that only equal ones count; from memory, rarely.
+template <typename T>
+__device__ __noinline__ float huge_terms(const TopShared<T>& sh, int j0, float top, int lane) {
+    const Slice<T>& S = sh.S;
+    float s = top == INFINITY ? NAN : 0.f;
+#pragma unroll 1
+    for (int i = 0; i < S.depth; ++i)
+        for (int e = 0; e < Row<T>::N; ++e) {
+            const int j = j0 + i * 32 + lane, v = j * Row<T>::N - S.shift + e;
+            if (j < S.v1 && v >= 0 && v < S.V) s += huge_term(Row<T>::wide(S.row[v]), top);
+        }
+    return s;
+}
+
+// Elements equal to x, in token order, until the buffer holds k: what is left of a list when nothing else comes before
+// them.  Called by the whole CTA.
+template <typename T>
+__device__ __noinline__ void fill_with(TopShared<T>& sh, float x, int k, int tid) {
+    const Slice<T>& S = sh.S;
+    const int lane = tid & 31, warp = tid >> 5, e0 = max(0, S.v0 * Row<T>::N - S.shift), e1 = min(S.V, S.v1 * Row<T>::N - S.shift);
+    int turn = 0, n = sh.count;
+#pragma unroll 1
+    for (int v0 = e0; v0 < e1 && n < k; v0 += NT) {
+        const int v = v0 + tid;
+        const bool on = v < e1 && Row<T>::wide(S.row[v]) == x;
+        const unsigned who = __ballot_sync(0xffffffffu, on);
+        int at = n + __popc(who & ((1u << lane) - 1u));
+        const int* all = sh.wcount[turn ^= 1];
+        n += block_count(on ? 1 : 0, sh.wcount[turn], lane, warp);
+        for (int w = 0; w < warp; ++w) at += all[w];
+        if (on && at < k) sh.buf[at] = full_key(x, v);
+    }
+    __syncthreads();
+    if (tid == 0) sh.count = min(n, k);
+    __syncthreads();
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_constant__ TopParams P) {
+    constexpr int N = Row<T>::N;
+    extern __shared__ __align__(16) unsigned char raw[];
+    TopShared<T>& sh = *reinterpret_cast<TopShared<T>*>(raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int row_id = blockIdx.x / P.cluster;
     if (P.scores) {                                 // beam selection: beams that offer nothing of their row
         const float s = P.scores[row_id];
         if (!(s > -INFINITY && s < INFINITY) || (P.finished && P.finished[row_id])) return;      // the whole cluster
     }
-    const T* row = static_cast<const T*>(P.x) + outer * P.outer_stride + in * P.row_stride;
-    const int V = P.V, k = P.k, shift = row_shift(row), nvec = row_vectors<T>(shift, V);
-    const int per = (nvec + C - 1) / C, v0 = min(nvec, (int)rank * per), v1 = min(nvec, v0 + per);
-    const f2 hi2 = sd::pack2(P.c.hi, P.c.hi), lo2 = sd::pack2(P.c.lo, P.c.lo);
+    if (tid == 0) {
+        const int outer = row_id / P.inner, in = row_id - outer * P.inner;
+        sh.S = Slice<T>(static_cast<const T*>(P.x) + outer * P.outer_stride + in * P.row_stride, P.V, P.cluster, blockIdx.x - row_id * P.cluster);
+        sh.count = sh.n_list = 0;
+    }
+    __syncthreads();
 
-    Part run{0.0, -INFINITY};                       // the same in every thread
-    int n_list = 0, cur = 0;
-    for (int t0 = v0; t0 < v1; t0 += TILE) {
-        uint4 r[NV];
-        load_tile<T>(row, shift, V, t0, v1, tid, r);
-        float m = vec_max(r[0], T());
+    double sum = 0.0;                               // of this thread's terms, against its warp's largest value
+    float top = -INFINITY;
+    {
+        const Slice<T>& S = sh.S;
+        // how many of the k largest the first chunks should hold, and some more
+        const int steps = S.steps(), own_steps = S.chunks_of(warp), stride = 32 * S.depth;
+        const float share = (float)P.k / (float)max(steps, 1);
+        int want = steps > 1 ? min(P.k, (int)(share + 3.5f * sqrtf(share)) + 2) : P.k;
+        const int real = min(S.V, S.v1 * N - S.shift) - max(0, S.v0 * N - S.shift);
+        float above = -INFINITY;                    // elements must be larger than this, too; those equal to it come last
+        bool strict = false;
+        for (int attempt = 0;; ++attempt) {
+            float bound = above;
+            int kept = 0;                               // vectors of this warp that reach the bound
+            int j0 = S.start(S.first_chunk(warp));
+            if (own_steps > 0) S.fetch(j0, lane, sh.chunk[warp]);
+            for (int step = 0; step == 0 || step < own_steps; ++step, j0 += stride) {
+                chunk_wait();
+                uint4 r[NV];
 #pragma unroll
-        for (int i = 1; i < NV; ++i) m = max_nan(m, vec_max(r[i], T()));
-        const float m_num = m == m ? m : -INFINITY;
-        const int active = min(WARPS, (v1 - t0 + 31) / 32), rth = (k + active - 1) / active;   // warps that hold a part of the tile
-        const float wm = warp_max(m_num), wr = warp_rth_largest(m_num, rth, lane);
-        if (lane == 0) { sh.wmax[warp] = wm; sh.wrth[warp] = wr; }
-        if (tid < n_list) sh.buf[tid] = sh.list[cur][tid];
-        if (tid == 0) sh.count = n_list;
-        __syncthreads();
-        float bound = sh.wrth[0], tm = sh.wmax[0];
-        for (int w = 1; w < active; ++w) { bound = fminf(bound, sh.wrth[w]); tm = fmaxf(tm, sh.wmax[w]); }
-        if (n_list == k) {                          // a full list from earlier tiles bounds this one as well
-            const uint32_t least = (uint32_t)(sh.list[cur][k - 1] >> 32);
-            if (least) bound = fmaxf(bound, key_value(least));
-        }
-        const float ref = reference(tm);
-        f2 acc = sd::pack2(0.f, 0.f);
-        const f2 neg = sd::pack2(-ref, -ref);
+                for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
+                Max<T> mx{r[0]};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            f2 x[N / 2];
-            pairs(r[i], x, T());
-            acc = sd::add2(acc, terms<N / 2>(x, neg, hi2, lo2));
-        }
-        const double ws = warp_sum((double)fold2(acc));
-        if (lane == 0) sh.wsum[warp] = ws;
-        if (!(m < bound)) {                         // NaN always passes: its key ranks it last
+                for (int i = 1; i < NV; ++i) mx = Max<T>{mx, Max<T>{r[i]}};
+                const float m = own_steps > 0 ? mx.value() : -INFINITY;
+                if (step == 0) {
+                    sh.tmax[tid] = m == m ? m : -INFINITY;
+                    __syncthreads();
+                    if (warp == 0) {                    // while the others sum their terms
+                        const float b = rth_of_maxima(sh.tmax, want, lane);
+                        if (lane == 0) sh.first_bound = b;
+                    }
+                }
+                if (step + 1 < own_steps) S.fetch(j0 + stride, lane, sh.chunk[warp]);        // this one is in registers
+                if (own_steps > 0 && attempt == 0) {
+                    const float wm = warp_max(m == m ? m : -INFINITY);
+                    if (wm > top) {
+                        sum *= (double)move_terms(top, wm, P.c);         // 0 so far where top is -inf
+                        top = wm;
+                    }
+                    if (ordinary(top) || top == -INFINITY) {
+                        const float u = reference(top) * P.c;
+                        const f2 neg = sd::pack2(-u, -u), c2 = sd::pack2(P.c, P.c);
+                        f2 acc = sd::pack2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (vec_max(r[i], T()) < bound) continue;
-                const int j = t0 + i * THREADS + tid;
-                float x[N];
-                widen<T>(r[i], x);
+                        for (int i = 0; i < NV; ++i) {
+                            f2 x[N / 2];
+                            pairs(r[i], x, T());
+                            acc = sd::add2(acc, terms<N / 2>(x, c2, neg));
+                        }
+                        sum += (double)fold2(acc);
+                    } else {
+                        sum += (double)huge_terms(sh, j0, top, lane);
+                    }
+                }
+                if (step == 0) {
+                    __syncthreads();
+                    if (!strict) {
+                        bound = above = sh.first_bound;
+                        strict = above == -INFINITY;    // a masked row: nothing to be gained from the -inf
+                    }
+                    if (strict) bound = key_value(min(value_key(above) + 1, 0xff800000u));       // the next float
+                }
+                if (__any_sync(0xffffffffu, !(m < bound))) {             // by NaN, too
+                    const Reach<T> reaches(bound);
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int v = j * N - shift + e;
-                    if (!(x[e] < bound) && j < v1 && v >= 0 && v < V) {
-                        const int pos = atomicAdd(&sh.count, 1);
-                        if (pos < CAP) sh.buf[pos] = full_key(x[e], v);
+                    for (int i = 0; i < NV; ++i) {
+                        const bool on = reaches(Max<T>{r[i]});       // never what lies outside the row: the bound is above -inf
+                        const unsigned who = __ballot_sync(0xffffffffu, on);
+                        if (who) {
+                            const int at = kept + __popc(who & ((1u << lane) - 1u));
+                            if (on && at < KEEP) {
+                                sh.vec[warp][at] = r[i];
+                                sh.vec_at[warp][at] = j0 + i * 32 + lane;
+                            }
+                            kept += __popc(who);
+                        }
                     }
                 }
             }
-        }
-        __syncthreads();
-        int n = sh.count;
-        if (n > CAP) {
-            const int t1 = min(v1, t0 + TILE);
-            const int real = min(V, t1 * N - shift) - max(0, t0 * N - shift);
-            __syncthreads();                        // everyone has read the count
-            if (tid == 0) sh.count = n_list;
+            // ---- the list.  NaN, which ranks last, is left to the careful pass
+            __syncwarp();
+            const int kept_elements = min(kept, KEEP) * N;
+            int reach = 0;
+            for (int p0 = 0; p0 < kept_elements; p0 += 32)
+                reach += __popc(__ballot_sync(0xffffffffu, p0 + lane < kept_elements && Row<T>::wide(reinterpret_cast<const T*>(sh.vec[warp])[p0 + lane]) >= bound));
+            int to = 0;
+            if (lane == 0 && reach) to = atomicAdd(&sh.count, reach);
+            to = __shfl_sync(0xffffffffu, to, 0);
+            for (int p0 = 0; p0 < kept_elements; p0 += 32) {
+                const int p = p0 + lane;
+                const bool is = p < kept_elements;
+                const float x = is ? Row<T>::wide(reinterpret_cast<const T*>(sh.vec[warp])[p]) : 0.f;
+                const unsigned who = __ballot_sync(0xffffffffu, is && x >= bound);
+                if (is && x >= bound) {
+                    const int v = sh.vec_at[warp][p / N] * N - S.shift + p % N, at = to + __popc(who & ((1u << lane) - 1u));
+                    if (at < CAP) sh.buf[at] = full_key(x, v);
+                }
+                to += __popc(who);
+            }
+            const bool lost = __syncthreads_or(kept > KEEP) || sh.count > CAP;
+            if (!lost && strict && sh.count < min(P.k, real)) fill_with(sh, above, min(P.k, real), tid);
+            const int n = sh.count;
             __syncthreads();
-            exact_select<T>(r, shift, V, t0, v1, min(k, real), sh, tid);
+            if (!lost && n >= min(P.k, real)) {
+                if (n > 0) rank_buffer(sh, n, P.k, tid);
+                break;
+            }
+            if (attempt == 1 || (lost && strict)) {
+                careful_pass(sh, P.k, tid);
+                break;
+            }
+            // too much for the lists: ties with the bound, most likely, so only what exceeds it; too little: a lower one
+            if (lost) strict = true;
+            else want = min(P.k, (int)(share + 6.f * sqrtf(share)) + 8);
+            if (tid == 0) sh.count = 0;
             __syncthreads();
-            n = sh.count;
         }
-        for (int i = tid; i < n; i += THREADS) {
-            const unsigned long long key = sh.buf[i];
-            int place = 0;
-            for (int q = 0; q < n; ++q) place += sh.buf[q] > key;
-            if (place < k) sh.list[cur ^ 1][place] = key;
-        }
-        double s = 0.0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) s += sh.wsum[w];
-        const float to = fmaxf(run.m, tm);
-        run.s = run.s * rescale(run.m, to, P.log2e_t) + s * rescale(tm, to, P.log2e_t);
-        run.m = to;
-        n_list = min(k, n);
-        cur ^= 1;
-        __syncthreads();
     }
 
-    if (C > 1) {
+    // ---- the row's sum
+    const int C = P.cluster, k = P.k, n_list = sh.n_list;
+    const uint32_t rank = blockIdx.x - row_id * C;
+    {
+        const float wm = warp_max(top);
+        if (lane == 0) sh.wmax[warp] = wm;
+        __syncthreads();
+        float all = sh.wmax[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) all = fmaxf(all, sh.wmax[w]);
+        sum = warp_sum(sum * (double)move_terms(top, all, P.c));
+        if (lane == 0) sh.wsum[warp] = sum;
+        __syncthreads();
         if (tid == 0) {
-            // the other CTAs find the finished list in list[0]
-            sh.n_list = n_list;
-            sh.part = run;
+            double s = 0.0;
+            for (int w = 0; w < NW; ++w) s += sh.wsum[w];
+            sh.part = Part{s * unround(reference(all), P.c), all};
         }
-        if (cur == 1 && tid < n_list) sh.list[0][tid] = sh.list[1][tid];
+    }
+    unsigned long long* lists = reinterpret_cast<unsigned long long*>(sh.chunk);      // of the other CTAs, MAX_TOP apart
+    if (C > 1) {
         sd::cl_sync();
-        for (int q = tid; q < C * MAX_TOP; q += THREADS) {
+        for (int q = tid; q < C * MAX_TOP; q += NT) {
             const uint32_t from = q / MAX_TOP;
             const int i = q - from * MAX_TOP;
-            if (from != rank && i < cl_ld_s32(&sh.n_list, from)) sh.buf[q] = cl_ld_u64(&sh.list[0][i], from);
+            if (from != rank && i < cl_ld_s32(&sh.n_list, from)) lists[q] = cl_ld_u64(&sh.list[i], from);
         }
-        if (rank == 0 && tid == 0) {
+        if (tid < C) sh.wcount[0][tid] = cl_ld_s32(&sh.n_list, tid);
+    }
+    if (rank == 0 && tid == 0) {
+        Part run = sh.part;
+        if (C > 1) {
             float to = run.m;
             for (int q = 1; q < C; ++q) to = fmaxf(to, cl_ld_f32(&sh.part.m, q));
             double s = run.s * rescale(run.m, to, P.log2e_t);
             for (int q = 1; q < C; ++q) s += cl_ld_f64(&sh.part.s, q) * rescale(cl_ld_f32(&sh.part.m, q), to, P.log2e_t);
-            run.s = s;
-            run.m = to;
+            run = Part{s, to};
         }
-        if (tid < C) sh.wcount[0][tid] = cl_ld_s32(&sh.n_list, tid);
-        sd::cl_sync();                              // nobody leaves while its list may still be read
-        cur = 0;
-    }
-    if (rank == 0 && tid == 0) {
         if (P.lse) P.lse[row_id] = (float)((double)reference(run.m) / P.T + log(run.s));
         if (P.parts) P.parts[row_id] = run;
     }
+    if (C > 1) sd::cl_sync();                       // nobody leaves while its list may still be read
     if (tid < n_list) {
-        const unsigned long long key = sh.list[cur][tid];
+        const unsigned long long key = sh.list[tid];
         int place = tid;
         for (int q = 0; q < C; ++q) {
             if (q == (int)rank) continue;
             int a = 0, b = sh.wcount[0][q];         // entries of list q above this one: keys fall along it
             while (a < b) {
                 const int mid = (a + b) >> 1;
-                if (sh.buf[q * MAX_TOP + mid] > key) a = mid + 1; else b = mid;
+                if (lists[q * MAX_TOP + mid] > key) a = mid + 1; else b = mid;
             }
             place += a;
         }
@@ -300,12 +542,18 @@ __global__ void __launch_bounds__(THREADS, 2) top_logits_kernel(const __grid_con
     }
 }
 
+template <typename T>
+cudaError_t launch_as(const TopParams& p, cudaStream_t s) {
+    return rw::launch(top_logits_kernel<T>, p, p.rows, p.cluster, sizeof(TopShared<T>), s);
+}
+
 }  // namespace
 
 cudaError_t launch_top_logits(TopParams p, specdec_dtype dtype, int rows, int sm_count, cudaStream_t s) {
     const int n = dtype == SPECDEC_F32 ? 4 : 8;
-    p.cluster = rw::cluster_size(rows, (p.V + n - 1) / n, sm_count);
-    if (dtype == SPECDEC_F32) return rw::launch(top_logits_kernel<float>, p, rows, p.cluster, 0, s);
-    if (dtype == SPECDEC_BF16) return rw::launch(top_logits_kernel<__nv_bfloat16>, p, rows, p.cluster, 0, s);
-    return rw::launch(top_logits_kernel<__half>, p, rows, p.cluster, 0, s);
+    p.rows = rows;
+    p.cluster = rw::cluster_size(rows, (p.V + n - 1) / n, sm_count, 1);
+    if (dtype == SPECDEC_F32) return launch_as<float>(p, s);
+    if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, s);
+    return launch_as<__half>(p, s);
 }
