@@ -575,9 +575,8 @@ int distill(specdec_ctx* ctx, const char* who, DistillMode mode, const specdec_d
     p.lse = r->lse;
     p.V = r->V;
     p.k = r->top_k;
-    p.T = (double)r->temperature;
-    p.log2e_t = 1.4426950408889634074 / p.T;
-    p.c = (float)p.log2e_t;
+    p.inv_t = 1.0 / (double)r->temperature;
+    p.c = (float)(1.4426950408889634074 / (double)r->temperature);
     p.loss = loss;
     p.saved = saved;
     p.weight = weight;

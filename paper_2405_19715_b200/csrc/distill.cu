@@ -14,11 +14,12 @@
 // the list, and the difference would keep few digits.  A bitmap of the CTA's part of the row tells list from rest.
 // sum p, R and the loss are in 64 bits for the same reason; they are a few values per listed token.
 //
-// A row is spread over a cluster of up to 8 CTAs, a warp holding 256 16-byte vectors (4 KB) of it in registers: its terms
-// are summed, the sums of all warps meet through distributed shared memory, and the gradient is formed from the same
-// registers: one read and one write of the row.  Rows that are longer than the cluster's registers are walked in chunks and
-// read a second time.  A listed token belongs to the CTA that has its logit, which adds its part to the sums and corrects
-// its gradient.
+// The 8 warps of a CTA have a stretch of the row each, and go through it in chunks of 4 KB, the next one on its way into
+// shared memory meanwhile: once for the terms' sums, and a step goes back over it, from the chunk that is still in
+// registers, for the gradient.  Rows are cut over the CTAs of a cluster until those that are worked on at one time fit L2
+// twice over, so that the way back reads no memory: one read and one write of the row.  Sums meet through distributed
+// shared memory, one record a warp.  A listed token belongs to the CTA that has its logit, which adds its part to the
+// sums and corrects its gradient.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -27,11 +28,10 @@ namespace {
 
 using namespace rw;
 
-constexpr int PER_SM = 4;
 
 // What a warp adds to the row's sums.
 struct Record {
-    double e, f, g;                                 // of its listed tokens: sum e, sum e L (see below), sum e (z - z_ref)
+    double e, h;                                    // of its listed tokens: sum e, sum e (L - (z - z_ref)/T), see below
     float s_out, s_in, m;                           // terms outside and inside the list, against m
     float z_ref;
     int flags;                                      // 1: a token that is none, or listed twice; 2: the list has an entry
@@ -42,8 +42,8 @@ struct DistillShared {
     Record record[NW];
     float wmax[NW];
     // of the row, once the records have met
-    float m, scale;
-    double mass, s, e;
+    float m, scale, inv_s;                          // inv_s: of the terms against the rounded m*c, as scale
+    double mass, e;
     int zero;
 };
 
@@ -59,29 +59,20 @@ __device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_one(__half* p, float v) { *p = __float2half_rn(v); }
 
-// Elements [j*N - shift, ... + N) of the gradient row; one 16-byte store where they lie inside the row and `wide` says
-// that the gradient row has the alignment of the logit row.
+// A vector of the gradient.  Streaming: what a step has still to read stays in L2 in its place.
 template <typename T>
-__device__ __forceinline__ void store_vec(T* row, int shift, int V, int j, bool wide, const float (&g)[Row<T>::N]) {
-    constexpr int N = Row<T>::N;
-    const int e0 = j * N - shift;
-    if (wide && e0 >= 0 && e0 + N <= V) {
-        uint4 w;
-        if constexpr (N == 4) w = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-        else w = make_uint4(store_pair(g[0], g[1], T()), store_pair(g[2], g[3], T()), store_pair(g[4], g[5], T()), store_pair(g[6], g[7], T()));
-        *reinterpret_cast<uint4*>(row + e0) = w;
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e0 + e >= 0 && e0 + e < V) store_one(row + e0 + e, g[e]);
-    }
+__device__ __forceinline__ void store_vec(T* to, const float (&g)[Row<T>::N]) {
+    uint4 w;
+    if constexpr (Row<T>::N == 4) w = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    else w = make_uint4(store_pair(g[0], g[1], T()), store_pair(g[2], g[3], T()), store_pair(g[4], g[5], T()), store_pair(g[6], g[7], T()));
+    __stcs(reinterpret_cast<uint4*>(to), w);
 }
 
-// Bits of the bitmap that belong to vector j of the slice.
+// Bits of the bitmap that belong to vector j of the slice: a byte for 8 elements, half of one for 4.
 template <typename T>
 __device__ __forceinline__ unsigned listed_bits(const uint32_t* bitmap, int j) {
-    const int bit = j * Row<T>::N;
-    return (bitmap[bit >> 5] >> (bit & 31)) & ((1u << Row<T>::N) - 1u);
+    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(bitmap);
+    return Row<T>::N == 8 ? bytes[j] : bytes[j >> 1] >> (4 * (j & 1)) & 15u;
 }
 
 // The same for logits so large that only those equal to the largest count; from memory, rarely.
@@ -98,108 +89,112 @@ __device__ __noinline__ void huge_terms(const Slice<T>& S, const uint32_t* bitma
 }
 
 template <typename T, DistillMode MODE>
-__global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_constant__ DistillParams P) {
+__global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill_kernel(const __grid_constant__ DistillParams P) {
     constexpr int N = Row<T>::N;
     constexpr bool STATS = MODE != DistillMode::Gradient, GRAD = MODE != DistillMode::Loss;
     extern __shared__ __align__(16) unsigned char raw[];
     DistillShared& sh = *reinterpret_cast<DistillShared*>(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = P.k, C = P.cluster;
+    // the list is the last warps' work, who have a chunk less than the first where the chunks do not come out even
+    const int list0 = NT - 1 - tid;
+    const bool lists = (NW - 1 - warp) * 32 < k;    // warps with entries
     // one entry per listed token of this CTA, at the token's place in the list; an entry is its thread's alone
-    double* prob = reinterpret_cast<double*>(raw + sizeof(DistillShared));       // [k] e, then p
+    double* prob = reinterpret_cast<double*>(raw + sizeof(DistillShared));       // [k] e
     int* ids = reinterpret_cast<int*>(prob + k);                                 // [k] -1: not of this CTA
-    float* zs = reinterpret_cast<float*>(ids + k);                               // [k]
+    float* vs = reinterpret_cast<float*>(ids + k);                               // [k] v
+    float* zs = vs + k;                                                          // [k] z
     uint32_t* bitmap = reinterpret_cast<uint32_t*>(zs + k);                      // [slice_words] listed tokens of this CTA
     const int row_id = blockIdx.x / C;
     const uint32_t rank = blockIdx.x - row_id * C;
+    const int32_t* tokens = P.tokens + (size_t)row_id * k;
+    const float* values = P.values + (size_t)row_id * k;
+    // asked for before anything is computed
+    const int first_id = list0 < k ? tokens[list0] : -1;
+    const float first_v = list0 < k ? values[list0] : 0.f, lse = P.lse ? P.lse[row_id] : 0.f;
     const Slice<T> S(static_cast<const T*>(P.z) + row_id * P.z_stride, P.V, C, rank);
     const int own_steps = S.chunks_of(warp), stride = 32 * S.depth, j_first = S.start(S.first_chunk(warp));
     const float weight = GRAD ? P.weight[row_id] : 1.f;
 
+    T* grad = GRAD ? static_cast<T*>(P.grad) + row_id * P.g_stride : nullptr;
+    const bool straight = GRAD && row_shift(grad) == S.shift;    // vectors of the logits are vectors of the gradient
     bool zero = GRAD && weight == 0.f;              // the row takes no part
-    float m = 0.f;
-    double s = 1.0, mass = 0.0;
-    float scale = 0.f;                              // of q's term, outside the list
+    const bool skipped = zero;
+    float m = 0.f, inv_s = 1.f, scale = 0.f;        // q of a term, and the gradient of one outside the list
+    double mass = 0.0;
+    const double wt = (double)weight * P.inv_t;
     if (MODE == DistillMode::Gradient) {
         const float4 sv = *reinterpret_cast<const float4*>(P.saved + (size_t)row_id * 4);
         m = sv.x;
-        s = sv.y;
+        inv_s = sv.y;
         mass = sv.w;
         zero |= sv.w < 0.f;
-        scale = (float)((double)weight / P.T * (double)sv.z / s);
+        scale = (float)(wt * (double)sv.z) * inv_s;
     }
-    if (!zero && own_steps > 0) S.fetch(j_first, lane, sh.chunk[warp]);        // on its way while the list is read
+    constexpr bool TWICE = MODE == DistillMode::Step;
+    if (!zero && own_steps > 0) S.fetch(j_first, lane, sh.chunk[warp], TWICE); // on its way while the list is read
 
-    // ---- the list: e = exp(L), L = v/T - lse, or (v - the largest v)/T to be divided by the sum
-    double e_sum = 0.0, f_sum = 0.0;
+    // ---- the list: e = exp(L), L = v/T - lse, or (v - the largest v)/T, to be divided by the sum of e
     int flags = 0;
+    double norm = 0.0, e_sum = 0.0;
     if (!zero) {
         if (STATS)
             for (int i = tid; i < P.slice_words; i += NT) bitmap[i] = 0;
-        double norm;
         if (P.lse) {
-            norm = (double)P.lse[row_id];
+            norm = (double)lse;
             if (STATS) __syncthreads();             // the bitmap is empty
         } else {
             float v_max = -INFINITY;
-            for (int i = tid; i < k; i += NT)
-                if ((unsigned)P.tokens[(size_t)row_id * k + i] < (unsigned)P.V) v_max = fmaxf(v_max, P.values[(size_t)row_id * k + i]);
+            for (int i = list0; i < k; i += NT)
+                if ((unsigned)(i == list0 ? first_id : tokens[i]) < (unsigned)P.V) v_max = fmaxf(v_max, i == list0 ? first_v : values[i]);
             v_max = warp_max(v_max);
             if (lane == 0) sh.wmax[warp] = v_max;
             __syncthreads();
             for (int w = 0; w < NW; ++w) v_max = fmaxf(v_max, sh.wmax[w]);
-            norm = (double)v_max / P.T;
+            norm = (double)v_max * P.inv_t;
         }
-        for (int i = tid; i < k; i += NT) {
-            const int id = P.tokens[(size_t)row_id * k + i];
+        for (int i = list0; i < k; i += NT) {
+            const int id = i == list0 ? first_id : tokens[i];
+            const float v = i == list0 ? first_v : values[i];
             const bool in = id >= 0 && id < P.V;
             const int at = (id + S.shift) / N;      // its vector
             const bool own = in && at >= S.v0 && at < S.v1;
             flags |= (in ? 2 : 0) | (id >= P.V || id < -1 ? 1 : 0);
             ids[i] = own ? id : -1;
-            // a renormalised gradient needs the whole list's sum, and has no other CTA to ask
-            if (!own && !(MODE == DistillMode::Gradient && !P.lse && in)) continue;
-            const float v = P.values[(size_t)row_id * k + i];
-            const double L = (double)v / P.T - norm, e = v == -INFINITY ? 0.0 : exp(L);
-            e_sum += e;
-            if (e != 0.0) f_sum += e * L;           // not 0 * -inf
-            if (!own) continue;
-            prob[i] = e;
-            if (STATS) {
+            if (own && STATS) {
                 const int bit = id + S.shift - S.v0 * N;
                 flags |= (atomicOr(&bitmap[bit >> 5], 1u << (bit & 31)) >> (bit & 31)) & 1u;       // listed twice
             }
+            // a renormalised gradient needs the whole list's sum, and has no other CTA to ask
+            if (!own && !(!STATS && !P.lse && in)) continue;
+            const double e = v == -INFINITY ? 0.0 : exp((double)v * P.inv_t - norm);
+            e_sum += e;
+            if (!own) continue;
+            prob[i] = e;
+            vs[i] = v;
+            if (!STATS) zs[i] = Row<T>::wide(S.row[id]);
         }
+        if (lists) e_sum = warp_sum(e_sum);
     }
-    uint4 r[NV];
-    chunk_wait();
-    __syncthreads();                                // the bitmap is complete, and every warp's chunk is there
-#pragma unroll
-    for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
-    if (!zero)
-        for (int i = tid; i < k; i += NT)
-            if (const int id = ids[i]; id >= 0) {
-                const int e = id + S.shift - S.v0 * N;
-                zs[i] = Row<T>::wide(S.steps() == 1 ? reinterpret_cast<const T*>(sh.chunk)[e / (stride * N) * (CHUNK * N) + e % (stride * N)] : S.row[id]);
-            }
+    // the bitmap is complete; where there is nothing to sum, the listed logits are read: the gradient may lie on them
+    __syncthreads();
 
-    if (MODE == DistillMode::Gradient && S.steps() > 1) __syncthreads();       // the gradient may lie on the logits
+    uint4 r[NV];
+    float s_out = 0.f, s_in = 0.f, top = -INFINITY;              // this lane's terms outside and inside the list
     if (STATS && !zero) {
-        // ---- the draft's terms
-        float s_out = 0.f, s_in = 0.f, top = -INFINITY;
         int j0 = j_first;
         for (int step = 0; step < own_steps; ++step, j0 += stride) {
-            if (step > 0) {
-                S.fetch(j0, lane, sh.chunk[warp]);
-                chunk_wait();
+            chunk_wait();
 #pragma unroll
-                for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
-            }
+            for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
             Max<T> mx{r[0]};
 #pragma unroll
             for (int i = 1; i < NV; ++i) mx = Max<T>{mx, Max<T>{r[i]}};
             const float own = mx.value(), wm = warp_max(own == own ? own : -INFINITY);    // NaN is met in the sums
+            // the next chunk, or the one before, with which the way back begins: this one stays in registers
+            if (step + 1 < own_steps) S.fetch(j0 + stride, lane, sh.chunk[warp], TWICE);
+            else if (GRAD && step > 0 && straight && S.whole(j0)) S.fetch(j0 - stride, lane, sh.chunk[warp]);
             if (wm > top) {
-                const float f = move_terms(top, wm, P.c);            // the sums are 0 so far where top is -inf
+                const float f = move_terms(top, wm, P.c);        // the sums are 0 so far where top is -inf
                 s_out *= f;
                 s_in *= f;
                 top = wm;
@@ -213,19 +208,22 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
                 for (int i = 0; i < NV; ++i) {
                     f2 x[N / 2];
                     pairs(r[i], x, T());
-                    const unsigned bits = i < S.depth ? listed_bits<T>(bitmap, min(j0 + i * 32 + lane, S.v1 - 1) - S.v0) : 0u;
-                    if (bits == 0u) {
-                        acc = sd::add2(acc, terms<N / 2>(x, c2, neg));
-                    } else {
+                    const unsigned bits = listed_bits<T>(bitmap, j0 - S.v0 + lane + i * 32);      // what is no vector has terms of 0
+                    f2 e[N / 2];
+#pragma unroll
+                    for (int q = 0; q < N / 2; ++q) e[q] = term2(x[q], c2, neg);
+                    if (bits) {
 #pragma unroll
                         for (int q = 0; q < N / 2; ++q) {
                             float a, b;
-                            sd::unpack2(term2(x[q], c2, neg), a, b);
+                            sd::unpack2(e[q], a, b);
                             const bool la = bits >> (2 * q) & 1u, lb = bits >> (2 * q + 1) & 1u;
                             in += (la ? a : 0.f) + (lb ? b : 0.f);
-                            acc = sd::add2(acc, sd::pack2(la ? 0.f : a, lb ? 0.f : b));
+                            e[q] = sd::pack2(la ? 0.f : a, lb ? 0.f : b);
                         }
                     }
+                    if constexpr (N == 8) acc = sd::add2(acc, sd::add2(sd::add2(e[0], e[1]), sd::add2(e[2], e[3])));
+                    else acc = sd::add2(acc, sd::add2(e[0], e[1]));
                 }
                 s_out += fold2(acc);
                 s_in += in;
@@ -233,107 +231,105 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
                 huge_terms(S, bitmap, j0, top, lane, s_out, s_in);
             }
         }
+    }
+
+    // ---- this warp's listed tokens.  Differences of logits are formed first, whatever the logits' size
+    double h_sum = 0.0;
+    float z_ref = -INFINITY;
+    if (STATS && !zero && lists) {
+        for (int i = list0; i < k; i += NT)
+            if (ids[i] >= 0) {
+                zs[i] = Row<T>::wide(S.row[ids[i]]);             // just read, from L2
+                if (prob[i] != 0.0) z_ref = fmaxf(z_ref, zs[i]);
+            }
+        z_ref = reference(warp_max(z_ref));
+        for (int i = list0; i < k; i += NT)
+            if (ids[i] >= 0 && prob[i] != 0.0)      // not 0 * -inf
+                h_sum += prob[i] * ((double)vs[i] * P.inv_t - norm - ((double)zs[i] - (double)z_ref) * P.inv_t);
+        h_sum = warp_sum(h_sum);
+        flags = __reduce_or_sync(0xffffffffu, flags);
+    }
+
+    if (STATS && !zero) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             s_out += __shfl_xor_sync(0xffffffffu, s_out, o);
             s_in += __shfl_xor_sync(0xffffffffu, s_in, o);
         }
-        // ---- this warp's record.  Differences of logits are formed first, whatever the logits' size
-        double g_sum = 0.0;
-        float z_ref = -INFINITY;
-        if (warp * 32 < k) {
-            for (int i = tid; i < k; i += NT)
-                if (ids[i] >= 0 && prob[i] != 0.0) z_ref = fmaxf(z_ref, zs[i]);
-            z_ref = reference(warp_max(z_ref));
-            for (int i = tid; i < k; i += NT)
-                if (ids[i] >= 0 && prob[i] != 0.0) g_sum += prob[i] * ((double)zs[i] - (double)z_ref);
-            e_sum = warp_sum(e_sum);
-            f_sum = warp_sum(f_sum);
-            g_sum = warp_sum(g_sum);
-            flags = __reduce_or_sync(0xffffffffu, flags);
-        }
-        if (lane == 0) sh.record[warp] = Record{e_sum, f_sum, g_sum, s_out, s_in, top, z_ref, flags};
+        if (lane == 0) sh.record[warp] = Record{e_sum, h_sum, s_out, s_in, top, z_ref, flags};
         if (C > 1) sd::cl_sync(); else __syncthreads();
-        double plogp = 0.0, pz = 0.0, S_out = 0.0, R = 0.0;
-        if (warp == 0) {
-            // ---- the row's sums, by every CTA for itself; two records a lane
-            Record rec[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int q = h * 32 + lane;
-                rec[h] = Record{0.0, 0.0, 0.0, 0.f, 0.f, -INFINITY, 0.f, 0};
-                if (q < C * NW) {
-                    const Record* from = &sh.record[q % NW];
-                    const uint32_t at = q / NW;
-                    rec[h].s_out = cl_ld_f32(&from->s_out, at);
-                    rec[h].s_in = cl_ld_f32(&from->s_in, at);
-                    rec[h].m = cl_ld_f32(&from->m, at);
-                    if (q % NW * 32 < k) {
-                        rec[h].e = cl_ld_f64(&from->e, at);
-                        rec[h].f = cl_ld_f64(&from->f, at);
-                        rec[h].g = cl_ld_f64(&from->g, at);
-                        rec[h].z_ref = cl_ld_f32(&from->z_ref, at);
-                        rec[h].flags = cl_ld_s32(&from->flags, at);
-                    }
+        double h = 0.0, R = 0.0, p = 0.0;
+        float out = 0.f, in = 0.f;
+        if (warp == NW - 1) {
+            // ---- the row's sums, by every CTA for itself: two records a lane at most
+            float all = -INFINITY;
+            for (int q = lane; q < C * NW; q += 32) all = fmaxf(all, cl_ld_f32(&sh.record[q % NW].m, q / NW));
+            all = warp_max(all);
+            m = reference(all);
+            double e = 0.0;
+            flags = 0;
+            for (int q = lane; q < C * NW; q += 32) {
+                const Record* from = &sh.record[q % NW];
+                const uint32_t at = q / NW;
+                const float to = move_terms(cl_ld_f32(&from->m, at), all, P.c);
+                out += cl_ld_f32(&from->s_out, at) * to;
+                in += cl_ld_f32(&from->s_in, at) * to;
+                if ((NW - 1 - q % NW) * 32 < k) {
+                    const double e1 = cl_ld_f64(&from->e, at);
+                    e += e1;
+                    h += cl_ld_f64(&from->h, at) - (e1 != 0.0 ? e1 * ((double)cl_ld_f32(&from->z_ref, at) - (double)m) * P.inv_t : 0.0);
+                    flags |= cl_ld_s32(&from->flags, at);
                 }
             }
-            const float all = warp_max(fmaxf(rec[0].m, rec[1].m));
-            m = reference(all);
-            double out = 0.0, in = 0.0, e = 0.0, f = 0.0, g = 0.0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float to = move_terms(rec[h].m, all, P.c);
-                out += (double)(rec[h].s_out * to);
-                in += (double)(rec[h].s_in * to);
-                e += rec[h].e;
-                f += rec[h].f;
-                g += rec[h].g + (rec[h].e != 0.0 ? rec[h].e * ((double)rec[h].z_ref - (double)m) : 0.0);
+            for (int o = 16; o > 0; o >>= 1) {
+                out += __shfl_xor_sync(0xffffffffu, out, o);
+                in += __shfl_xor_sync(0xffffffffu, in, o);
             }
-            const double exact = unround(m, P.c);
-            S_out = warp_sum(out) * exact;
-            s = S_out + warp_sum(in) * exact;
             e = warp_sum(e);
-            plogp = warp_sum(f);
-            pz = warp_sum(g);
-            flags = __reduce_or_sync(0xffffffffu, rec[0].flags | rec[1].flags);
-            if (!P.lse) {                           // p = e / sum e
-                plogp = e > 0.0 ? plogp / e - log(e) : e;
-                pz = e > 0.0 ? pz / e : e;
-            }
-            const double p = P.lse ? e : e > 0.0 ? 1.0 : e;         // sum p; NaN stays NaN
-            R = P.lse && S_out > 0.0 ? fmax(0.0, 1.0 - p) : 0.0;     // a draft with nothing outside the list has no rest
+            flags = __reduce_or_sync(0xffffffffu, flags);
+            const float s = out + in;
+            p = P.lse ? e : e > 0.0 ? 1.0 : e;      // sum p; NaN stays NaN
+            R = P.lse && out > 0.f ? fmax(0.0, 1.0 - p) : 0.0;       // a draft with nothing outside the list has no rest
             mass = p + R;
-            const double out_factor = mass - (R > 0.0 ? R * s / S_out : 0.0);
-            zero = flags != 2 || s == 0.0;          // a bad list, an empty one, or no logit above -inf
+            const double out_factor = mass - (R > 0.0 ? R * (double)(s / out) : 0.0);
+            zero = flags != 2 || s == 0.f;          // a bad list, an empty one, or no logit above -inf
+            inv_s = 1.f / s;
             if (lane == 0) {
                 sh.m = m;
-                sh.s = s;
+                sh.inv_s = inv_s;
                 sh.mass = mass;
-                sh.e = P.lse || e == 0.0 ? 1.0 : e;         // what e is divided by; a list without mass stays one
-                sh.scale = (float)((double)weight / P.T * out_factor / (s / exact));       // of a term against the rounded m*c
+                sh.e = P.lse || e == 0.0 ? 1.0 : e; // what e is divided by; a list without mass stays one
+                sh.scale = (float)(wt * out_factor) * inv_s;
                 sh.zero = zero;
-                if (rank == 0) {
-                    float loss;
-                    if (flags & 1) loss = NAN;
-                    else if (flags == 0) loss = 0.f;
-                    else if (s == 0.0) loss = p > 0.0 ? INFINITY : 0.f;
-                    else {
-                        double l = plogp;
-                        if (p > 0.0) l += p * log(s) - pz / P.T;
-                        if (R > 0.0) l += R * (log(R) - log(S_out / s));
-                        loss = s == s ? (float)l : NAN;
-                    }
-                    P.loss[row_id] = loss;
-                    if (flags & 1) atomicOr(P.status, SPECDEC_DATA_BAD_TOKEN);
-                    if (MODE == DistillMode::Loss)
-                        *reinterpret_cast<float4*>(P.saved + (size_t)row_id * 4) = make_float4(m, (float)(s / exact), (float)out_factor, zero ? -1.f : (float)mass);
-                }
+                if (MODE == DistillMode::Loss && rank == 0)
+                    *reinterpret_cast<float4*>(P.saved + (size_t)row_id * 4) = make_float4(m, inv_s, (float)out_factor, zero ? -1.f : (float)mass);
             }
         }
-        if (C > 1) sd::cl_sync(); else __syncthreads();      // nobody leaves, or writes over logits, while others still read
-        if (!GRAD) return;
+        // nobody leaves while its records may still be read: arrived here, waited for at the end
+        if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        __syncthreads();
+        if (rank == 0 && warp == NW - 1) {
+            h = warp_sum(h);
+            if (lane == 0) {
+                const float s = out + in;
+                float loss;
+                if (flags & 1) loss = NAN;
+                else if (flags == 0) loss = 0.f;
+                else if (s == 0.f) loss = p > 0.0 ? INFINITY : 0.f;
+                else {
+                    // sum p (log p - (z - m)/T) + p log(sum exp((z - m)/T)); renormalised, p = e / sum e
+                    double l = P.lse ? h : p == 0.0 ? 0.0 : h / sh.e - log(sh.e);
+                    if (p > 0.0) l += p * log((double)s * unround(m, P.c));
+                    if (R > 0.0) l += R * log(R * (double)s / (double)out);
+                    loss = s == s ? (float)l : NAN;
+                }
+                P.loss[row_id] = loss;
+                if (flags & 1) atomicOr(P.status, SPECDEC_DATA_BAD_TOKEN);
+            }
+        }
         m = sh.m;
-        s = sh.s;
+        inv_s = sh.inv_s;
         mass = sh.mass;
         scale = sh.scale;
         zero = sh.zero;
@@ -341,12 +337,10 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
     } else if (STATS && rank == 0 && tid == 0) {    // a step of weight 0
         P.loss[row_id] = 0.f;
     }
+    const bool arrived = STATS && C > 1 && !skipped;
     if constexpr (GRAD) {
-        const float u = m * P.c;
         if (MODE == DistillMode::Gradient && !zero) {
-            s *= unround(m, P.c);                   // against m itself
             if (!P.lse) {                           // the list's sum
-                e_sum = warp_sum(e_sum);
                 if (lane == 0) sh.record[warp].e = e_sum;
                 __syncthreads();
                 e_sum = 0.0;
@@ -356,45 +350,63 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
                 e_sum = 1.0;
             }
         }
-        // ---- the gradient, from the chunk that the registers hold: the last one, or the first
-        T* grad = static_cast<T*>(P.grad) + row_id * P.g_stride;
-        const bool wide = row_shift(grad) == S.shift;
+        // ---- the gradient: a step goes back from the chunk that the registers hold
+        const float u = m * P.c;
         const f2 c2 = sd::pack2(P.c, P.c), neg = sd::pack2(-u, -u), scale2 = sd::pack2(scale, scale);
-        const bool normal = ordinary(m);
-        for (int n = 0; n < own_steps; ++n) {
-            const int j0 = j_first + (STATS ? own_steps - 1 - n : n) * stride;
-            if (!zero && n > 0) {
-                S.fetch(j0, lane, sh.chunk[warp]);
-                chunk_wait();
+        const bool plain = ordinary(m) && !zero;
+        const int back = STATS ? -stride : stride;
+        int j0 = STATS ? j_first + (own_steps - 1) * stride : j_first;
+        for (int n = 0; n < own_steps; ++n, j0 += back) {
+            const bool in_registers = STATS && n == 0;
+            if (!in_registers) chunk_wait();
+            if (plain && straight && S.whole(j0)) {
+                if (!in_registers) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int j = j0 + i * 32 + lane;
-                if (i >= S.depth || j >= S.v1) continue;
-                float g[N];
-                f2 x[N / 2];
-                pairs(r[i], x, T());
-#pragma unroll
-                for (int q = 0; q < N / 2; ++q) sd::unpack2(sd::mul2(term2(x[q], c2, neg), scale2), g[2 * q], g[2 * q + 1]);
-                if (!normal || zero) {
-                    widen<T>(r[i], g);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) g[e] = zero ? 0.f : huge_term(g[e], m) * scale;
+                    for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
+                    if (n + 1 < own_steps) S.fetch(j0 + back, lane, sh.chunk[warp]);
                 }
-                store_vec<T>(grad, S.shift, S.V, j, wide, g);
+                T* to = grad + ((long long)(j0 + lane) * N - S.shift);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float g[N];
+                    f2 x[N / 2];
+                    pairs(r[i], x, T());
+#pragma unroll
+                    for (int q = 0; q < N / 2; ++q) sd::unpack2(sd::mul2(term2(x[q], c2, neg), scale2), g[2 * q], g[2 * q + 1]);
+                    store_vec<T>(to + i * 32 * N, g);
+                }
+                continue;
             }
+            // the first and last chunk of a row at odd addresses, a gradient at others than the logits', rows without one
+#pragma unroll 1
+            for (int i = 0; i < S.depth; ++i) {
+                const int j = j0 + i * 32 + lane, e0 = j * N - S.shift;
+                if (j >= S.v1) break;
+                float g[N];
+                widen<T>(sh.chunk[warp][i * 32 + lane], g);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    g[e] = zero ? 0.f : (ordinary(m) ? sd::ex2(fmaf(g[e], P.c, -u)) : huge_term(g[e], m)) * scale;
+                if (straight && e0 >= 0 && e0 + N <= S.V) {
+                    store_vec<T>(grad + e0, g);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e0 + e >= 0 && e0 + e < S.V) store_one(grad + e0 + e, g[e]);
+                }
+            }
+            if (!zero && n + 1 < own_steps) S.fetch(j0 + back, lane, sh.chunk[warp]);
         }
-        if (zero) return;
-        __syncthreads();                            // the CTA's part is written: the listed tokens are written over
-        const double wt = (double)weight / P.T;
-        for (int i = tid; i < k; i += NT)
-            if (const int id = ids[i]; id >= 0) {
-                const double q = exp(((double)zs[i] - (double)m) / P.T) / s;
-                store_one(grad + id, (float)(wt * (mass * q - prob[i] / e_sum)));
-            }
+        if (!zero) {
+            __syncthreads();                        // the CTA's part is written: the listed tokens are written over
+            for (int i = list0; i < k; i += NT)
+                if (const int id = ids[i]; id >= 0) {
+                    const float q = (ordinary(m) ? sd::ex2(fmaf(zs[i], P.c, -u)) : huge_term(zs[i], m)) * inv_s;
+                    store_one(grad + id, (float)(wt * (mass * (double)q - prob[i] / e_sum)));
+                }
+        }
     }
+    if (arrived) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 template <typename T>
@@ -411,10 +423,13 @@ cudaError_t launch_as(const DistillParams& p, DistillMode mode, int rows, size_t
 cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mode, int rows, int sm_count, cudaStream_t s) {
     const int n = dtype == SPECDEC_F32 ? 4 : 8;
     const int most = (p.V + 2 * n - 2) / n;        // vectors of a row at its worst alignment
-    const int hold = NW * CHUNK;                   // vectors that a CTA's registers hold
-    p.cluster = rw::cluster_size(rows, most, sm_count, std::min(MAX_CLUSTER, (most + hold - 1) / hold));
-    p.slice_words = ((most + p.cluster - 1) / p.cluster * n + 31) / 32;
-    const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 16;
+    int least = 1;
+    // a step reads its rows twice: CTAs * row / cluster bytes at one time, in half of the 126 MB of L2
+    if (mode == DistillMode::Step)
+        while (least < MAX_CLUSTER && 3ll * sm_count / least * most * 16 > (64ll << 20)) least *= 2;
+    p.cluster = rw::cluster_size(rows, most, sm_count, least);
+    p.slice_words = (((most + p.cluster - 1) / p.cluster + CHUNK) * n + 31) / 32;      // whole chunks
+    const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 20;
     if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, smem, s);
     if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, smem, s);
     return launch_as<__half>(p, mode, rows, smem, s);

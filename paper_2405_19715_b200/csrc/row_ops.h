@@ -63,7 +63,7 @@ struct DistillParams {
     const float* lse;                         // null: renormalised over the list
     int V, k, cluster, slice_words;
     float c;                                  // log2(e) / T
-    double T, log2e_t;
+    double inv_t;
     float* loss;
     float* saved;                             // [rows, 4]: written by the loss alone, read by the gradient alone
     const float* weight;                      // [rows]: gradient of the result in each row's loss

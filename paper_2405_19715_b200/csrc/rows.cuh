@@ -168,18 +168,26 @@ struct Slice {
     __device__ __forceinline__ int chunks_of(int warp) const { return base + (warp < extra ? 1 : 0); }
     __device__ __forceinline__ int steps() const { return base + (extra ? 1 : 0); }      // of the warp that has most
     __device__ __forceinline__ int start(int chunk) const { return v0 + chunk * 32 * depth; }
+    // whether all of the chunk that starts at vector j0 lies inside the row
+    __device__ __forceinline__ bool whole(int j0) const { return depth == NV && j0 >= in0 && j0 + CHUNK <= in0 + in_n; }
     __device__ __forceinline__ bool inside(int j) const { return (unsigned)(j - in0) < (unsigned)in_n; }
     __device__ __forceinline__ const T* address(int j) const { return row + ((long long)j * Row<T>::N - shift); }
     // The copy into shared memory of the chunk that starts at vector j0, asynchronous: it costs no register while it is on
     // its way.  A lane reads back, after chunk_wait(), only what it has asked for itself: vector j0 + i * 32 + lane at
-    // buffer[i * 32 + lane].  -inf where there is no vector.
-    __device__ __forceinline__ void fetch(int j0, int lane, uint4* buffer) const {
+    // buffer[i * 32 + lane].  -inf where there is no vector.  `again`: the chunk will be read once more, and should stay
+    // in L2 meanwhile; otherwise it is the first to go.
+    __device__ __forceinline__ void fetch(int j0, int lane, uint4* buffer, bool again = false) const {
+        unsigned long long first, normal;
+        asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+        asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+        const unsigned long long policy = again ? normal : first;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(buffer + lane);
-        if (depth == NV && j0 >= in0 && j0 + CHUNK <= in0 + in_n) {
+        if (whole(j0)) {
             const T* p = address(j0 + lane);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(p + i * 32 * Row<T>::N) : "memory");
+                asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + i * 512), "l"(p + i * 32 * Row<T>::N), "l"(policy)
+                             : "memory");
         } else {
             const uint32_t w = Row<T>::neg_inf();
 #pragma unroll 1
@@ -229,7 +237,11 @@ __device__ __forceinline__ float move_terms(float from, float to, float c) {
     return from == to ? 1.f : ordinary(from) && ordinary(to) ? sd::ex2(from * c - to * c) : 0.f;
 }
 // The factor from sums against the rounded m*c to sums against m itself.
-__device__ __forceinline__ double unround(float m, float c) { return ordinary(m) ? exp2((double)(m * c) - (double)m * (double)c) : 1.0; }
+__device__ __forceinline__ double unround(float m, float c) {
+    if (!ordinary(m)) return 1.0;
+    const double x = (double)(m * c) - (double)m * (double)c, y = x * 0.69314718055994530942;
+    return y * y < 1e-8 ? 1.0 + y * (1.0 + y * (0.5 + y * (1.0 / 6.0))) : exp2(x);         // the series' next term: 4e-18
+}
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
 __device__ __forceinline__ double cl_ld_f64(const double* p, uint32_t rank) { return sd::cl_ld_f64(sd::cl_map(p, rank)); }
