@@ -470,8 +470,10 @@ int specdec_distill_step(specdec_ctx* ctx, const specdec_distill_rows* rows, con
  * Candidates are ranked in 64 bits; out_scores is rounded once.
  *   workspace   dev, 16-byte aligned, at least specdec_beam_workspace(B, W, V, n_out) bytes; its contents do not
  *               matter before the call or after it.  Calls that overlap on the GPU need a workspace each.
- * 1 <= n_out <= min(W*V, SPECDEC_TOP_LOGITS_MAX); W * min(n_out, V) <= SPECDEC_BEAM_MAX_CANDIDATES.
+ * W <= SPECDEC_BEAM_MAX_WIDTH; 1 <= n_out <= min(W*V, SPECDEC_TOP_LOGITS_MAX); W * min(n_out, V) <=
+ * SPECDEC_BEAM_MAX_CANDIDATES.
  */
+#define SPECDEC_BEAM_MAX_WIDTH 128
 #define SPECDEC_BEAM_MAX_CANDIDATES 8192
 size_t specdec_beam_workspace(int B, int W, int V, int n_out);
 int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int64_t batch_stride, int64_t beam_stride,
@@ -488,9 +490,8 @@ int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtyp
  *            as it is (in dst: a copy of itself); so does one >= W, which sets SPECDEC_DATA_BAD_PARENT.
  *   src, dst dev, the same strides in both; src == dst reorders in place, without any buffer.  A partial overlap, or
  *            strides that let two beams share a byte, are EINVAL.
- * W <= SPECDEC_BEAM_MAX_REORDER.
+ * W <= SPECDEC_BEAM_MAX_WIDTH.
  */
-#define SPECDEC_BEAM_MAX_REORDER 128
 typedef struct specdec_beam_state {
     const void* src;
     void* dst;

@@ -649,6 +649,7 @@ int specdec_beam_select(specdec_ctx* ctx, const void* logits, specdec_dtype dtyp
     if (!ctx) return SPECDEC_EINVAL;
     if (!logits || !scores || !out_scores || !out_parents || !out_tokens || !workspace) return fail(ctx, SPECDEC_EINVAL, "beam_select: null pointer argument");
     if (B < 1 || W < 1) return fail(ctx, SPECDEC_EINVAL, "beam_select: B and W must be >= 1 (got %d, %d)", B, W);
+    if (W > SPECDEC_BEAM_MAX_WIDTH) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_select: %d beams, above %d", W, SPECDEC_BEAM_MAX_WIDTH);
     if ((long long)B * W > ROWS_MAX) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_select: %lld beams, above 2^27", (long long)B * W);
     if (int rc = check_row_args(ctx, "beam_select", logits, (int)dtype, beam_stride, B * W, V, temperature)) return rc;
     if (batch_stride < 0 || (B > 1 && batch_stride < V)) return fail(ctx, SPECDEC_EINVAL, "beam_select: a batch stride of %lld elements", (long long)batch_stride);
@@ -710,7 +711,7 @@ int specdec_beam_reorder(specdec_ctx* ctx, const int32_t* parents, int64_t paren
     if (!parents || !state || !state->src || !state->dst) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: null pointer argument");
     if (B < 1 || W < 1 || state->outer < 1 || state->runs < 1 || state->steps < 1 || state->step_bytes < 1)
         return fail(ctx, SPECDEC_EINVAL, "beam_reorder: every extent must be >= 1");
-    if (W > SPECDEC_BEAM_MAX_REORDER) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_reorder: %d beams, above %d", W, SPECDEC_BEAM_MAX_REORDER);
+    if (W > SPECDEC_BEAM_MAX_WIDTH) return fail(ctx, SPECDEC_EUNSUPPORTED, "beam_reorder: %d beams, above %d", W, SPECDEC_BEAM_MAX_WIDTH);
     if (parent_stride < W) return fail(ctx, SPECDEC_EINVAL, "beam_reorder: a parent stride of %lld, below W=%d", (long long)parent_stride, W);
     // no two beams may share a byte: dimension by dimension from the smallest stride, each steps over all below it
     struct Dim { int64_t n, stride; } d[4] = {{state->outer, state->outer_stride}, {B, state->batch_stride}, {W, state->beam_stride}, {state->runs, state->run_stride}};

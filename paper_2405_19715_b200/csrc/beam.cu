@@ -22,53 +22,98 @@ __device__ __forceinline__ double key_score(unsigned long long key) {
 }
 __device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
 
+constexpr int FEW = 512;                         // candidates that are ranked as they are
+
 __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
     extern __shared__ __align__(16) unsigned char raw[];
     const int n = P.W * P.k;
-    unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // 0: no candidate
+    unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // [W][k], falling along a beam; 0: no candidate
     int* flat = reinterpret_cast<int*>(keys + n);                               // w * V + v
+    __shared__ int counts[MERGE_WARPS], dead[SPECDEC_BEAM_MAX_WIDTH / 32], survivors;
+    __shared__ unsigned long long bounds[8];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int mine = 0;
+    for (int w = tid; w < (P.W + 31) / 32; w += MERGE_THREADS) dead[w] = 0;
+    if (tid < 8) bounds[tid] = 0;
+    if (tid == 0) survivors = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");             // the row kernel's lists
+    __syncthreads();
     for (int w = warp; w < P.W; w += MERGE_WARPS) {
         const int row = b * P.W + w;
+        // of an ended or empty beam parts and lists hold nothing: asked for all the same, so that nothing waits in turn
         const float s = P.scores[row];
         const bool ended = P.finished && P.finished[row], live = s > -INFINITY && s < INFINITY;
-        double lse = 0.0;
-        bool open = live && !ended;
-        if (open) {
-            const Part part = P.parts[row];
-            lse = (double)reference(part.m) / P.T + log(part.s);
-            open = is_finite(lse);                  // a row without a finite sum offers nothing
-        }
+        const Part part = P.parts[row];
+        const double lse = (double)reference(part.m) / P.T + log(part.s);
+        const bool open = live && !ended && is_finite(lse);        // a row without a finite sum offers nothing
+        if (!ended && !open && lane == 0) atomicOr(&dead[w / 32], 1 << w % 32);
         for (int i = lane; i < P.k; i += 32) {
             const int o = w * P.k + i;
-            unsigned long long key = 0;
-            int v = 0;
-            if (ended) {
-                if (i == 0) key = score_key(live ? (double)s : -INFINITY);
-                v = P.end_token;
-            } else if (open) {
-                v = P.tokens[(size_t)row * P.k + i];
-                key = score_key((double)s + ((double)P.values[(size_t)row * P.k + i] / P.T - lse));
-            } else {                                // every candidate has -inf: the lowest tokens come first
-                v = i;
-                key = score_key(-INFINITY);
-            }
-            keys[o] = key;
-            flat[o] = w * P.V + v;
-            mine += key != 0;
+            const float x = P.values[(size_t)row * P.k + i];
+            const int token = P.tokens[(size_t)row * P.k + i];
+            // an empty beam's candidates all have -inf: the lowest tokens come first
+            keys[o] = ended ? (i ? 0ull : score_key(live ? (double)s : -INFINITY)) : score_key(open ? (double)s + ((double)x / P.T - lse) : -INFINITY);
+            flat[o] = w * P.V + (ended ? P.end_token : open ? token : i);
+        }
+    }
+    __syncthreads();
+    int mine = 0;
+    for (int w = warp; w < P.W; w += MERGE_WARPS) {
+        // of several empty beams the first has all that can be chosen, unless its vocabulary is smaller than n_out
+        bool first = true;
+        for (int q = 0; q <= w / 32; ++q) first &= (dead[q] & (q < w / 32 ? ~0 : (1 << w % 32) - 1)) == 0;
+        const bool drop = (dead[w / 32] >> w % 32 & 1) && !first && P.k == P.M;
+        for (int i = lane; i < P.k; i += 32) {
+            if (drop) keys[w * P.k + i] = 0;
+            mine += keys[w * P.k + i] != 0 ? 1 : 0;
         }
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
-    __shared__ int counts[MERGE_WARPS];
     if (lane == 0) counts[warp] = mine;
     __syncthreads();
-    for (int i = tid; i < n; i += MERGE_THREADS) {
-        const unsigned long long key = keys[i];
-        if (key == 0) continue;
-        const int f = flat[i];
+    int total = 0;
+    for (int w = 0; w < MERGE_WARPS; ++w) total += counts[w];
+
+    unsigned long long bound = 1;                   // of the candidates that can be among the M best
+    if (n > FEW && warp < 8) {
+        // Where h beams have r + 1 candidates at or above a value, (r + 1) h do: for r = 0, 1, 3, ... 127 the h-th largest
+        // of the beams' r-th candidates, h = M / (r + 1) rounded up, is a bound
+        const int r = (1 << warp) - 1, h = (P.M + r) / (r + 1);
+        if (r < P.k && h <= P.W)
+            for (int w = lane; w < P.W; w += 32) {
+                const unsigned long long key = keys[w * P.k + r];
+                int above = 0, same = 0;
+                for (int q = 0; q < P.W; ++q) {
+                    above += keys[q * P.k + r] > key ? 1 : 0;
+                    same += keys[q * P.k + r] == key ? 1 : 0;
+                }
+                if (above < h && above + same >= h) bounds[warp] = key;      // the same from every lane that gets here
+            }
+    }
+    if (n > FEW) {
+        __syncthreads();
+        for (int q = 0; q < 8; ++q) bound = bounds[q] > bound ? bounds[q] : bound;
+    }
+    // survivors are listed behind the arrays: a candidate's place is counted among them
+    int* list = flat + n;
+    for (int i0 = 0; i0 < n; i0 += MERGE_THREADS) {
+        const int i = i0 + tid;
+        const bool on = i < n && keys[i] >= bound;
+        const unsigned who = __ballot_sync(0xffffffffu, on);
+        int at = 0;
+        if (lane == 0 && who) at = atomicAdd(&survivors, __popc(who));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+        if (on) list[at] = i;
+    }
+    __syncthreads();
+    const int left = survivors;
+    for (int i = tid; i < left; i += MERGE_THREADS) {
+        const unsigned long long key = keys[list[i]];
+        const int f = flat[list[i]];
         int place = 0;
-        for (int q = 0; q < n; ++q) place += keys[q] > key || (keys[q] == key && flat[q] < f);
+        for (int q = 0; q < left; ++q) {
+            const int o = list[q];
+            place += keys[o] > key || (keys[o] == key && flat[o] < f) ? 1 : 0;
+        }
         if (place < P.M) {
             const size_t o = (size_t)b * P.M + place;
             P.out_scores[o] = (float)key_score(key);
@@ -76,9 +121,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
             P.out_tokens[o] = f % P.V;
         }
     }
-    int total = 0;
-    for (int w = 0; w < MERGE_WARPS; ++w) total += counts[w];
-    for (int i = total + tid; i < P.M; i += MERGE_THREADS) {          // fewer candidates than places
+    for (int i = total + tid; i < P.M; i += MERGE_THREADS) {       // fewer candidates than places
         const size_t o = (size_t)b * P.M + i;
         P.out_scores[o] = -INFINITY;
         P.out_parents[o] = -1;
@@ -217,7 +260,7 @@ cudaError_t reorder_as(const ReorderParams& p, cudaStream_t s) {
 
 }  // namespace
 
-size_t beam_merge_smem(int W, int k) { return (size_t)W * k * (sizeof(unsigned long long) + sizeof(int)); }
+size_t beam_merge_smem(int W, int k) { return (size_t)W * k * (sizeof(unsigned long long) + 2 * sizeof(int)); }
 
 cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s) {
     const size_t smem = beam_merge_smem(p.W, p.k);
@@ -225,8 +268,18 @@ cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s) {
         const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    beam_merge_kernel<<<B, MERGE_THREADS, smem, s>>>(p);
-    return cudaGetLastError();
+    // launched while the row kernel still runs; the kernel waits for it
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)B);
+    cfg.blockDim = dim3(MERGE_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = a;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, beam_merge_kernel, p);
 }
 
 cudaError_t launch_beam_reorder(const ReorderParams& p, cudaStream_t s) {

@@ -409,12 +409,17 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
     if (arrived) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+template <typename T, DistillMode MODE>
+cudaError_t launch_one(const DistillParams& p, int rows, size_t smem, cudaStream_t s) {
+    static std::atomic<unsigned long long> allowed{0};
+    return rw::launch(distill_kernel<T, MODE>, allowed, p, rows, p.cluster, smem, s);
+}
 template <typename T>
 cudaError_t launch_as(const DistillParams& p, DistillMode mode, int rows, size_t smem, cudaStream_t s) {
     switch (mode) {
-        case DistillMode::Loss: return rw::launch(distill_kernel<T, DistillMode::Loss>, p, rows, p.cluster, smem, s);
-        case DistillMode::Gradient: return rw::launch(distill_kernel<T, DistillMode::Gradient>, p, rows, p.cluster, smem, s);
-        default: return rw::launch(distill_kernel<T, DistillMode::Step>, p, rows, p.cluster, smem, s);
+        case DistillMode::Loss: return launch_one<T, DistillMode::Loss>(p, rows, smem, s);
+        case DistillMode::Gradient: return launch_one<T, DistillMode::Gradient>(p, rows, smem, s);
+        default: return launch_one<T, DistillMode::Step>(p, rows, smem, s);
     }
 }
 

@@ -3,6 +3,8 @@
 // split of a row over the CTAs of a thread-block cluster.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_fp16.h>
 
 #include "row_ops.h"
@@ -15,6 +17,7 @@ using sd::f2;
 constexpr int NT = 256, NW = NT / 32;          // threads of a CTA
 constexpr int NV = 8;                          // 16-byte vectors a thread holds: 32 registers
 constexpr int MAX_CLUSTER = 8;
+constexpr int MAX_SMEM = 227 * 1024;           // of a CTA
 
 template <typename T> struct Row;
 template <> struct Row<float> {
@@ -264,11 +267,19 @@ inline int cluster_size(long long rows, int nvec, int sm_count, int least) {
     return C;
 }
 
+// `allowed`, one per kernel: the devices (by bit) on which it may use more than the default 48 KB of shared memory.
 template <typename P>
-inline cudaError_t launch(void (*kernel)(P), const P& p, long long clusters, int C, size_t smem, cudaStream_t s) {
+inline cudaError_t launch(void (*kernel)(P), std::atomic<unsigned long long>& allowed, const P& p, long long clusters, int C, size_t smem, cudaStream_t s) {
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
         if (e != cudaSuccess) return e;
+        const unsigned long long bit = device < 64 ? 1ull << device : 0ull;
+        if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+            if (e != cudaSuccess) return e;
+            allowed.fetch_or(bit, std::memory_order_relaxed);
+        }
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * C));

@@ -26,16 +26,16 @@ constexpr int CAP = 2048;                  // elements in the buffer
 constexpr int KEEP = 96;                   // vectors a warp can keep
 constexpr int PER_SM = 3;                  // CTAs of an SM; a fourth would leave 64 registers, and measured 10 % slower
 static_assert(MAX_TOP <= NT && CAP >= 2 * MAX_TOP && CAP % NT == 0, "the lists fit the buffer");
-static_assert(MAX_CLUSTER * MAX_TOP * 8 <= NW * CHUNK * 16, "the lists of a cluster fit the chunks");
+static_assert(MAX_CLUSTER <= NW && MAX_TOP * 8 <= CHUNK * 16, "a warp for every list, with room for it");
 
 // Everything that all threads share lives here, the row's geometry among it: the registers of a thread hold its vectors.
 template <typename T>
 struct TopShared {
     Slice<T> S;
-    uint4 chunk[NW][CHUNK];                // each warp's coming chunk; at the end the lists of the cluster
+    uint4 chunk[NW][CHUNK];                // each warp's coming chunk; at the end the list of another CTA
     union {
         uint4 vec[NW][KEEP];
-        int place[CAP];                    // of the buffer's entries, while they are ranked
+        int place[CAP];                    // of the buffer's entries while they are ranked, of the list's in the cluster
     };
     int vec_at[NW][KEEP];                  // which vector of the row it is
     unsigned long long buf[CAP];
@@ -45,7 +45,7 @@ struct TopShared {
     int wcount[2][NW];
     int count, n_list;                     // elements in the buffer (or that would be), length of the list
     float first_bound;
-    Part part;
+    Part part, whole;                      // of the CTA, of the cluster
 };
 
 // The r-th largest of the 256 thread maxima, or a value just below it (its key's leading 16 bits); -inf if fewer are
@@ -479,72 +479,69 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
         }
     }
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // beam selection's second kernel may take its place
+
     // ---- the row's sum
-    const int C = P.cluster, k = P.k, n_list = sh.n_list;
-    const uint32_t rank = blockIdx.x - row_id * C;
-    {
-        const float wm = warp_max(top);
-        if (lane == 0) sh.wmax[warp] = wm;
-        __syncthreads();
-        float all = sh.wmax[0];
+    const int C = P.cluster, k = P.k, n_list = sh.n_list, rank = blockIdx.x - row_id * C;
+    if (lane == 0) sh.wmax[warp] = top;
+    if (tid < n_list) sh.place[tid] = tid;
+    __syncthreads();
+    float all = sh.wmax[0];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) all = fmaxf(all, sh.wmax[w]);
-        sum = warp_sum(sum * (double)move_terms(top, all, P.c));
-        if (lane == 0) sh.wsum[warp] = sum;
-        __syncthreads();
-        if (tid == 0) {
-            double s = 0.0;
-            for (int w = 0; w < NW; ++w) s += sh.wsum[w];
-            sh.part = Part{s * unround(reference(all), P.c), all};
-        }
+    for (int w = 1; w < NW; ++w) all = fmaxf(all, sh.wmax[w]);
+    sum = warp_sum(sum * (double)move_terms(top, all, P.c));
+    if (lane == 0) sh.wsum[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        double s = 0.0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) s += sh.wsum[w];
+        sh.part = Part{s * unround(reference(all), P.c), all};
     }
-    unsigned long long* lists = reinterpret_cast<unsigned long long*>(sh.chunk);      // of the other CTAs, MAX_TOP apart
     if (C > 1) {
+        // ---- every warp but one compares this CTA's list with that of another; the one adds up the CTAs' sums
         sd::cl_sync();
-        for (int q = tid; q < C * MAX_TOP; q += NT) {
-            const uint32_t from = q / MAX_TOP;
-            const int i = q - from * MAX_TOP;
-            if (from != rank && i < cl_ld_s32(&sh.n_list, from)) lists[q] = cl_ld_u64(&sh.list[i], from);
+        if (warp < C && warp != rank) {
+            unsigned long long* theirs = reinterpret_cast<unsigned long long*>(sh.chunk[warp]);
+            const int n = cl_ld_s32(&sh.n_list, warp);
+            for (int i = lane; i < n; i += 32) theirs[i] = cl_ld_u64(&sh.list[i], warp);
+            __syncwarp();
+            for (int i = lane; i < n_list; i += 32) {
+                const unsigned long long key = sh.list[i];
+                int a = 0, b = n;                   // entries of theirs above this one: keys fall along a list
+                while (a < b) {
+                    const int mid = (a + b) >> 1;
+                    if (theirs[mid] > key) a = mid + 1; else b = mid;
+                }
+                if (a) atomicAdd(&sh.place[i], a);
+            }
         }
-        if (tid < C) sh.wcount[0][tid] = cl_ld_s32(&sh.n_list, tid);
+        if (warp == rank) {
+            const float m = lane < C ? cl_ld_f32(&sh.part.m, lane) : -INFINITY, to = warp_max(m);
+            const double s = warp_sum(lane < C ? cl_ld_f64(&sh.part.s, lane) * rescale(m, to, P.log2e_t) : 0.0);
+            if (lane == 0) sh.whole = Part{s, to};
+        }
+        __syncthreads();
     }
     if (rank == 0 && tid == 0) {
-        Part run = sh.part;
-        if (C > 1) {
-            float to = run.m;
-            for (int q = 1; q < C; ++q) to = fmaxf(to, cl_ld_f32(&sh.part.m, q));
-            double s = run.s * rescale(run.m, to, P.log2e_t);
-            for (int q = 1; q < C; ++q) s += cl_ld_f64(&sh.part.s, q) * rescale(cl_ld_f32(&sh.part.m, q), to, P.log2e_t);
-            run = Part{s, to};
-        }
+        const Part run = C > 1 ? sh.whole : sh.part;
         if (P.lse) P.lse[row_id] = (float)((double)reference(run.m) / P.T + log(run.s));
         if (P.parts) P.parts[row_id] = run;
     }
-    if (C > 1) sd::cl_sync();                       // nobody leaves while its list may still be read
-    if (tid < n_list) {
+    if (tid < n_list && sh.place[tid] < k) {
         const unsigned long long key = sh.list[tid];
-        int place = tid;
-        for (int q = 0; q < C; ++q) {
-            if (q == (int)rank) continue;
-            int a = 0, b = sh.wcount[0][q];         // entries of list q above this one: keys fall along it
-            while (a < b) {
-                const int mid = (a + b) >> 1;
-                if (lists[q * MAX_TOP + mid] > key) a = mid + 1; else b = mid;
-            }
-            place += a;
-        }
-        if (place < k) {
-            const size_t o = (size_t)row_id * k + place;
-            const uint32_t vk = (uint32_t)(key >> 32);
-            P.values[o] = vk ? key_value(vk) : __int_as_float(0x7fffffff);
-            P.tokens[o] = key_token(key);
-        }
+        const size_t o = (size_t)row_id * k + sh.place[tid];
+        const uint32_t vk = (uint32_t)(key >> 32);
+        P.values[o] = vk ? key_value(vk) : __int_as_float(0x7fffffff);
+        P.tokens[o] = key_token(key);
     }
+    if (C > 1) sd::cl_sync();                       // nobody leaves while its list may still be read
 }
 
 template <typename T>
 cudaError_t launch_as(const TopParams& p, cudaStream_t s) {
-    return rw::launch(top_logits_kernel<T>, p, p.rows, p.cluster, sizeof(TopShared<T>), s);
+    static std::atomic<unsigned long long> allowed{0};
+    return rw::launch(top_logits_kernel<T>, allowed, p, p.rows, p.cluster, sizeof(TopShared<T>), s);
 }
 
 }  // namespace

@@ -29,7 +29,7 @@ SHARD_STATS_WIDTH, SHARD_MAX_RANKS = 8, 64
 STATIC_MAX_UNITS, STATIC_MAX_V = 16384, 262144
 STAMP_SLOTS = 32
 TOP_LOGITS_MAX, DISTILL_MAX_LIST, DISTILL_SAVED = 256, 1024, 4
-BEAM_MAX_CANDIDATES, BEAM_MAX_REORDER = 8192, 128
+BEAM_MAX_CANDIDATES, BEAM_MAX_WIDTH = 8192, 128
 
 
 class SpecdecError(RuntimeError):
@@ -446,15 +446,15 @@ def _row_dtype(t: torch.Tensor) -> int:
     return _ROW_DTYPES[t.dtype]
 
 
-def _on(ctx: Context, *tensors):
-    """Every tensor lives on the context's GPU: its pointers mean nothing to another."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != ctx.device):
-            raise ValueError(f"tensor is on {t.device}, the context on cuda:{ctx.device}")
+def _here(ctx: Context, t: torch.Tensor) -> torch.Tensor:
+    """The tensor lives on the context's GPU: its pointer means nothing to another."""
+    if t.get_device() != ctx.device:                # -1 for a host tensor
+        raise ValueError(f"tensor is on {t.device}, the context on cuda:{ctx.device}")
+    return t
 
 
-def _row_stream(ctx: Context, stream):
-    return stream if stream is not None else torch.cuda.current_stream(ctx.device)
+def _row_stream(ctx: Context, stream) -> int:
+    return (stream if stream is not None else torch.cuda.current_stream(ctx.device)).cuda_stream
 
 
 def _empty(ctx: Context, stream, shape, dtype):
@@ -465,59 +465,63 @@ def _empty(ctx: Context, stream, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=ctx.device)
 
 
-def _rows_of(t: torch.Tensor, V: int | None = None):
-    """(pointer, row stride) of a [rows, V] tensor whose rows' elements follow one another."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+def _rows_of(ctx: Context, t: torch.Tensor):
+    """(pointer, row stride, rows, V) of a [rows, V] tensor whose rows' elements follow one another."""
+    _here(ctx, t)
+    if t.dim() != 2:
+        raise ValueError("expected [rows, V]")
+    rows, V = t.shape
+    stride, inner = t.stride()
+    if V > 1 and inner != 1:
         raise ValueError("expected [rows, V] with adjacent elements in a row")
-    if V is not None and t.shape[1] != V:
-        raise ValueError(f"expected rows of {V}, got {t.shape[1]}")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return t.data_ptr(), (stride if rows > 1 else V), rows, V
 
 
-def _shaped(t: torch.Tensor | None, shape, dtype):
-    """Pointer of a contiguous tensor of this shape and type."""
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _ptr(t, dtype)
+def _arg(ctx: Context, t: torch.Tensor | None, shape: tuple, dtype) -> int | None:
+    """Pointer of a contiguous tensor of this shape and type on the context's GPU."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    return _here(ctx, t).data_ptr()
 
 
 def specdec_top_logits(ctx: Context, logits, top_k: int, temperature: float = 1.0, values=None, tokens=None, lse=None,
                        stream=None):
     """specdec_top_logits of the C ABI: logits [rows, V] -> (values [rows, k] f32, tokens [rows, k] int32, lse [rows] f32)."""
-    _on(ctx, logits, values, tokens, lse)
-    ptr, stride = _rows_of(logits)
-    (rows, V), k = logits.shape, int(top_k)
+    ptr, stride, rows, V = _rows_of(ctx, logits)
+    k = int(top_k)
     if values is None:
         values = _empty(ctx, stream, (rows, k), torch.float32)
     if tokens is None:
         tokens = _empty(ctx, stream, (rows, k), torch.int32)
     if lse is None:
         lse = _empty(ctx, stream, (rows,), torch.float32)
-    ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, float(temperature),
-                                          _shaped(values, (rows, k), torch.float32), _shaped(tokens, (rows, k), torch.int32),
-                                          _shaped(lse, (rows,), torch.float32), _row_stream(ctx, stream).cuda_stream))
+    ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, temperature,
+                                          _arg(ctx, values, (rows, k), torch.float32), _arg(ctx, tokens, (rows, k), torch.int32),
+                                          _arg(ctx, lse, (rows,), torch.float32), _row_stream(ctx, stream)))
     return values, tokens, lse
 
 
 def _distill_rows(ctx, logits, values, tokens, lse, temperature):
-    _on(ctx, logits, values, tokens, lse)
-    ptr, stride = _rows_of(logits)
-    rows, V = logits.shape
+    ptr, stride, rows, V = _rows_of(ctx, logits)
     if values.dim() != 2:
         raise ValueError("values must be [rows, k]")
     k = values.shape[1]
-    return _DistillRows(ptr, _row_dtype(logits), stride, _shaped(values, (rows, k), torch.float32),
-                        _shaped(tokens, (rows, k), torch.int32), _shaped(lse, (rows,), torch.float32), rows, V, k,
-                        float(temperature))
+    return _DistillRows(ptr, _row_dtype(logits), stride, _arg(ctx, values, (rows, k), torch.float32),
+                        _arg(ctx, tokens, (rows, k), torch.int32), _arg(ctx, lse, (rows,), torch.float32), rows, V, k,
+                        temperature)
 
 
 def _gradient(ctx, stream, logits, grad):
+    """(gradient, pointer, row stride): laid out like the logits unless given, so that both have the same alignment."""
     if grad is None:
-        grad = _empty(ctx, stream, tuple(logits.shape), logits.dtype)
-    _on(ctx, grad)
-    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        rows, V = logits.shape
+        stride = logits.stride(0) if rows > 1 else V
+        grad = _empty(ctx, stream, (rows, max(stride, V)), logits.dtype)[:, :V]
+    elif grad.dtype != logits.dtype or grad.shape != logits.shape:
         raise ValueError("the gradient must have the shape and type of the logits")
-    return grad, *_rows_of(grad)
+    return grad, *_rows_of(ctx, grad)[:2]
 
 
 def specdec_distill(ctx: Context, logits, values, tokens, lse, temperature: float = 1.0, loss=None, saved=None,
@@ -525,42 +529,39 @@ def specdec_distill(ctx: Context, logits, values, tokens, lse, temperature: floa
     """specdec_distill of the C ABI: draft logits [rows, V] against the target's record (values, tokens [rows, k]; lse
     [rows], or None to renormalise over the list) -> (loss [rows] f32, saved for specdec_distill_backward)."""
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
-    _on(ctx, loss, saved)
+    n = r.rows
     if loss is None:
-        loss = _empty(ctx, stream, (r.rows,), torch.float32)
+        loss = _empty(ctx, stream, (n,), torch.float32)
     if saved is None:
-        saved = _empty(ctx, stream, (r.rows, DISTILL_SAVED), torch.float32)
-    ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), _shaped(loss, (r.rows,), torch.float32),
-                                       _shaped(saved, (r.rows, DISTILL_SAVED), torch.float32),
-                                       _row_stream(ctx, stream).cuda_stream))
+        saved = _empty(ctx, stream, (n, DISTILL_SAVED), torch.float32)
+    ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), _arg(ctx, loss, (n,), torch.float32),
+                                       _arg(ctx, saved, (n, DISTILL_SAVED), torch.float32), _row_stream(ctx, stream)))
     return loss, saved
 
 
 def specdec_distill_backward(ctx: Context, logits, values, tokens, lse, saved, row_grad, temperature: float = 1.0,
                              grad=None, stream=None):
     """specdec_distill_backward of the C ABI: gradient [rows, V] of sum_n row_grad[n] * loss[n] in the draft logits, of
-    their type; `grad` may be `logits` itself."""
+    their type and row stride; `grad` may be `logits` itself."""
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
-    _on(ctx, saved, row_grad)
     grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
-    ctx._check(ctx.lib.specdec_distill_backward(ctx.handle, C.byref(r), _shaped(saved, (r.rows, DISTILL_SAVED), torch.float32),
-                                                _shaped(row_grad, (r.rows,), torch.float32), gptr, gstride,
-                                                _row_stream(ctx, stream).cuda_stream))
+    ctx._check(ctx.lib.specdec_distill_backward(ctx.handle, C.byref(r), _arg(ctx, saved, (r.rows, DISTILL_SAVED), torch.float32),
+                                                _arg(ctx, row_grad, (r.rows,), torch.float32), gptr, gstride,
+                                                _row_stream(ctx, stream)))
     return grad
 
 
 def specdec_distill_step(ctx: Context, logits, values, tokens, lse, row_weight, temperature: float = 1.0, loss=None,
                          grad=None, stream=None):
-    """specdec_distill_step of the C ABI: (loss [rows], gradient [rows, V] of sum_n row_weight[n] * loss[n]) in one pass;
-    `grad` may be `logits` itself."""
+    """specdec_distill_step of the C ABI: (loss [rows], gradient [rows, V] of sum_n row_weight[n] * loss[n]) in one pass, the
+    gradient of the logits' type and row stride; `grad` may be `logits` itself."""
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
-    _on(ctx, row_weight, loss)
+    n = r.rows
     if loss is None:
-        loss = _empty(ctx, stream, (r.rows,), torch.float32)
+        loss = _empty(ctx, stream, (n,), torch.float32)
     grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
-    ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _shaped(row_weight, (r.rows,), torch.float32),
-                                            _shaped(loss, (r.rows,), torch.float32), gptr, gstride,
-                                            _row_stream(ctx, stream).cuda_stream))
+    ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _arg(ctx, row_weight, (n,), torch.float32),
+                                            _arg(ctx, loss, (n,), torch.float32), gptr, gstride, _row_stream(ctx, stream)))
     return loss, grad
 
 
@@ -569,8 +570,7 @@ def specdec_beam_select(ctx: Context, logits, scores, n_out: int, temperature: f
     """specdec_beam_select of the C ABI: logits [B, W, V], scores [B, W] f32, finished [B, W] int32 or None ->
     (scores [B, n_out] f32, parents [B, n_out] int32, tokens [B, n_out] int32).  The workspace (uint8, at least
     specdec_beam_workspace bytes) is allocated here unless passed in."""
-    _on(ctx, logits, scores, finished, out_scores, parents, tokens, workspace)
-    if logits.dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
+    if _here(ctx, logits).dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
         raise ValueError("logits must be [B, W, V] with adjacent elements in a row")
     B, W, V = logits.shape
     M = int(n_out)
@@ -583,12 +583,12 @@ def specdec_beam_select(ctx: Context, logits, scores, n_out: int, temperature: f
     if tokens is None:
         tokens = _empty(ctx, stream, (B, M), torch.int32)
     if workspace is None:
-        workspace = _empty(ctx, stream, (ctx.lib.specdec_beam_workspace(B, W, V, M),), torch.uint8)
+        workspace = _empty(ctx, stream, ctx.lib.specdec_beam_workspace(B, W, V, M), torch.uint8)
     ctx._check(ctx.lib.specdec_beam_select(
-        ctx.handle, logits.data_ptr(), _row_dtype(logits), batch_stride, beam_stride, _shaped(scores, (B, W), torch.float32),
-        _shaped(finished, (B, W), torch.int32), int(end_token), float(temperature), B, W, V, M,
-        _shaped(out_scores, (B, M), torch.float32), _shaped(parents, (B, M), torch.int32), _shaped(tokens, (B, M), torch.int32),
-        _ptr(workspace, torch.uint8), workspace.numel(), _row_stream(ctx, stream).cuda_stream))
+        ctx.handle, logits.data_ptr(), _row_dtype(logits), batch_stride, beam_stride, _arg(ctx, scores, (B, W), torch.float32),
+        _arg(ctx, finished, (B, W), torch.int32), end_token, temperature, B, W, V, M,
+        _arg(ctx, out_scores, (B, M), torch.float32), _arg(ctx, parents, (B, M), torch.int32), _arg(ctx, tokens, (B, M), torch.int32),
+        _arg(ctx, workspace, workspace.shape, torch.uint8), workspace.numel(), _row_stream(ctx, stream)))
     return out_scores, parents, tokens
 
 
@@ -639,7 +639,8 @@ def specdec_beam_reorder(ctx: Context, parents, state, batch_dim: int = 0, step_
     be strided).  `state` has the entries at batch_dim and the beams behind it; with step_dim only the first lens[b]
     (int32 [B]) steps move.  In place unless `out`, of the same shape and strides, is given.  Returns the reordered state."""
     dst = state if out is None else out
-    _on(ctx, parents, state, dst, lens)
+    for t in (parents, state, dst):
+        _here(ctx, t)
     if dst.shape != state.shape or dst.dtype != state.dtype or dst.stride() != state.stride():
         raise ValueError("out must have the shape, strides and type of the state")
     if state.numel() == 0:
@@ -652,6 +653,6 @@ def specdec_beam_reorder(ctx: Context, parents, state, batch_dim: int = 0, step_
         raise ValueError("lens needs step_dim")
     st = _BeamState(state.data_ptr(), dst.data_ptr(), *layout)
     ctx._check(ctx.lib.specdec_beam_reorder(ctx.handle, parents.data_ptr(), parents.stride(0) if B > 1 else W,
-                                            _shaped(lens, (B,), torch.int32), B, W, C.byref(st),
-                                            _row_stream(ctx, stream).cuda_stream))
+                                            _arg(ctx, lens, (B,), torch.int32), B, W, C.byref(st),
+                                            _row_stream(ctx, stream)))
     return dst
