@@ -127,7 +127,7 @@ __device__ __noinline__ void rank_buffer(TopShared<T>& sh, int n, int k, int tid
             key[e] = i0 + e * 32 + lane < n ? sh.buf[i0 + e * 32 + lane] : ~0ull;
             place[e] = 0;
         }
-#pragma unroll 2
+#pragma unroll 4
         for (int q = q0; q < q1; ++q) {
             const unsigned long long x = sh.buf[q];
 #pragma unroll
@@ -443,11 +443,13 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
             __syncwarp();
             const int kept_elements = min(kept, KEEP) * N;
             int reach = 0;
+#pragma unroll 4
             for (int p0 = 0; p0 < kept_elements; p0 += 32)
                 reach += __popc(__ballot_sync(0xffffffffu, p0 + lane < kept_elements && Row<T>::wide(reinterpret_cast<const T*>(sh.vec[warp])[p0 + lane]) >= bound));
             int to = 0;
             if (lane == 0 && reach) to = atomicAdd(&sh.count, reach);
             to = __shfl_sync(0xffffffffu, to, 0);
+#pragma unroll 2
             for (int p0 = 0; p0 < kept_elements; p0 += 32) {
                 const int p = p0 + lane;
                 const bool is = p < kept_elements;

@@ -453,16 +453,21 @@ def _here(ctx: Context, t: torch.Tensor) -> torch.Tensor:
     return t
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle alone, without a Stream object around it
+
+
 def _row_stream(ctx: Context, stream) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(ctx.device)).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(ctx.device) if _raw_stream is not None else torch.cuda.current_stream(ctx.device).cuda_stream
 
 
-def _empty(ctx: Context, stream, shape, dtype):
-    """A tensor of the stream that the call runs on (the allocator hands memory out by stream)."""
+def _empty(like: torch.Tensor, stream, shape, dtype):
+    """A tensor on the GPU of `like`, of the stream that the call runs on (the allocator hands memory out by stream)."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=ctx.device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=ctx.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _rows_of(ctx: Context, t: torch.Tensor):
@@ -492,11 +497,11 @@ def specdec_top_logits(ctx: Context, logits, top_k: int, temperature: float = 1.
     ptr, stride, rows, V = _rows_of(ctx, logits)
     k = int(top_k)
     if values is None:
-        values = _empty(ctx, stream, (rows, k), torch.float32)
+        values = _empty(logits, stream, (rows, k), torch.float32)
     if tokens is None:
-        tokens = _empty(ctx, stream, (rows, k), torch.int32)
+        tokens = _empty(logits, stream, (rows, k), torch.int32)
     if lse is None:
-        lse = _empty(ctx, stream, (rows,), torch.float32)
+        lse = _empty(logits, stream, (rows,), torch.float32)
     ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, temperature,
                                           _arg(ctx, values, (rows, k), torch.float32), _arg(ctx, tokens, (rows, k), torch.int32),
                                           _arg(ctx, lse, (rows,), torch.float32), _row_stream(ctx, stream)))
@@ -518,7 +523,7 @@ def _gradient(ctx, stream, logits, grad):
     if grad is None:
         rows, V = logits.shape
         stride = logits.stride(0) if rows > 1 else V
-        grad = _empty(ctx, stream, (rows, max(stride, V)), logits.dtype)[:, :V]
+        grad = _empty(logits, stream, (rows, max(stride, V)), logits.dtype)[:, :V]
     elif grad.dtype != logits.dtype or grad.shape != logits.shape:
         raise ValueError("the gradient must have the shape and type of the logits")
     return grad, *_rows_of(ctx, grad)[:2]
@@ -531,9 +536,9 @@ def specdec_distill(ctx: Context, logits, values, tokens, lse, temperature: floa
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
     n = r.rows
     if loss is None:
-        loss = _empty(ctx, stream, (n,), torch.float32)
+        loss = _empty(logits, stream, (n,), torch.float32)
     if saved is None:
-        saved = _empty(ctx, stream, (n, DISTILL_SAVED), torch.float32)
+        saved = _empty(logits, stream, (n, DISTILL_SAVED), torch.float32)
     ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), _arg(ctx, loss, (n,), torch.float32),
                                        _arg(ctx, saved, (n, DISTILL_SAVED), torch.float32), _row_stream(ctx, stream)))
     return loss, saved
@@ -558,7 +563,7 @@ def specdec_distill_step(ctx: Context, logits, values, tokens, lse, row_weight, 
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
     n = r.rows
     if loss is None:
-        loss = _empty(ctx, stream, (n,), torch.float32)
+        loss = _empty(logits, stream, (n,), torch.float32)
     grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
     ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _arg(ctx, row_weight, (n,), torch.float32),
                                             _arg(ctx, loss, (n,), torch.float32), gptr, gstride, _row_stream(ctx, stream)))
@@ -577,13 +582,13 @@ def specdec_beam_select(ctx: Context, logits, scores, n_out: int, temperature: f
     beam_stride = logits.stride(1) if W > 1 else V
     batch_stride = logits.stride(0) if B > 1 else V
     if out_scores is None:
-        out_scores = _empty(ctx, stream, (B, M), torch.float32)
+        out_scores = _empty(logits, stream, (B, M), torch.float32)
     if parents is None:
-        parents = _empty(ctx, stream, (B, M), torch.int32)
+        parents = _empty(logits, stream, (B, M), torch.int32)
     if tokens is None:
-        tokens = _empty(ctx, stream, (B, M), torch.int32)
+        tokens = _empty(logits, stream, (B, M), torch.int32)
     if workspace is None:
-        workspace = _empty(ctx, stream, ctx.lib.specdec_beam_workspace(B, W, V, M), torch.uint8)
+        workspace = _empty(logits, stream, ctx.lib.specdec_beam_workspace(B, W, V, M), torch.uint8)
     ctx._check(ctx.lib.specdec_beam_select(
         ctx.handle, logits.data_ptr(), _row_dtype(logits), batch_stride, beam_stride, _arg(ctx, scores, (B, W), torch.float32),
         _arg(ctx, finished, (B, W), torch.int32), end_token, temperature, B, W, V, M,
