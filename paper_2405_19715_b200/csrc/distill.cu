@@ -377,7 +377,9 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                 }
                 continue;
             }
-            // the first and last chunk of a row at odd addresses, a gradient at others than the logits', rows without one
+            // the first and last chunk of a row at odd addresses, rows without a gradient, a gradient at addresses of
+            // another alignment than the logits': that goes back through shared memory, to be stored element next to element
+            T* const staged = reinterpret_cast<T*>(sh.chunk[warp]);
 #pragma unroll 1
             for (int i = 0; i < S.depth; ++i) {
                 const int j = j0 + i * 32 + lane, e0 = j * N - S.shift;
@@ -391,9 +393,18 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                     store_vec<T>(grad + e0, g);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e0 + e >= 0 && e0 + e < S.V) store_one(grad + e0 + e, g[e]);
+                    for (int e = 0; e < N; ++e) {
+                        if (!straight) store_one(staged + (i * 32 + lane) * N + e, g[e]);
+                        else if (e0 + e >= 0 && e0 + e < S.V) store_one(grad + e0 + e, g[e]);
+                    }
                 }
+            }
+            if (!straight) {
+                __syncwarp();
+                const int e0 = j0 * N - S.shift, end = min(stride, S.v1 - j0) * N;
+                for (int e = lane; e < end; e += 32)
+                    if (e0 + e >= 0 && e0 + e < S.V) grad[e0 + e] = staged[e];
+                __syncwarp();
             }
             if (!zero && n + 1 < own_steps) S.fetch(j0 + back, lane, sh.chunk[warp]);
         }
@@ -434,8 +445,11 @@ cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mod
     // 44 us with one, 47 us with two
     if (mode == DistillMode::Step)
         while (least < MAX_CLUSTER && std::min<long long>(rows, 3ll * sm_count / least) * most * 16 > (80ll << 20)) least *= 2;
+    // the bitmap of a CTA's part takes at most 128 KB of shared memory
+    if (mode != DistillMode::Gradient)
+        while (least < MAX_CLUSTER && (most / least + CHUNK) * n > (128 << 13)) least *= 2;
     p.cluster = rw::cluster_size(rows, most, 2 * sm_count, least);
-    p.slice_words = (((most + p.cluster - 1) / p.cluster + CHUNK) * n + 31) / 32;      // whole chunks
+    p.slice_words = mode == DistillMode::Gradient ? 0 : (((most + p.cluster - 1) / p.cluster + CHUNK) * n + 31) / 32;      // whole chunks
     const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 20;
     if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, smem, s);
     if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, smem, s);

@@ -186,6 +186,34 @@ def test_distill(ctx, n, V, k, T, dtype, rest):
     _run_all(ctx, z, values, tokens, lse, w, T, dtype)
 
 
+def test_distill_lists_longer_than_the_vocabulary_and_of_one_token(ctx):
+    """k beyond V, its other entries empty; lists of the longest kind; a row with one entry at the end of its list."""
+    z, values, tokens, lse, w = _record(2, 5, 9, 9, "bf16", 1.0, True)
+    values = torch.cat([values, torch.full((5, 31), float("nan"), device="cuda")], 1).contiguous()
+    tokens = torch.cat([tokens, torch.full((5, 31), -1, dtype=torch.int32, device="cuda")], 1).contiguous()
+    tokens[2, :8] = -1
+    _run_all(ctx, z, values, tokens, lse, w, 1.0, "bf16")
+    _run_all(ctx, z, values, tokens, None, w, 1.0, "bf16")
+    z, values, tokens, lse, w = _record(3, 3, 5003, 1024, "f32", 1.0, True)
+    tokens[1, :1000] = -1
+    tokens[2, :1023] = -1
+    _run_all(ctx, z, values, tokens, lse, w, 1.0, "f32")
+    _run_all(ctx, z, values, tokens, None, w, 1.0, "f32")
+
+
+@pytest.mark.parametrize("dtype,n,V", [("f32", 2, 1 << 22), ("bf16", 2, (1 << 22) - 3), ("f16", 60, 500001)])
+def test_the_largest_vocabularies(ctx, dtype, n, V):
+    z, values, tokens, lse, w = _record(6, n, V, 40, dtype, 1.0, True)
+    loss, grad = specdec.specdec_distill_step(ctx, z, values, tokens, lse, w, 1.0)
+    loss1, saved = specdec.specdec_distill(ctx, z, values, tokens, lse, 1.0)
+    grad1 = specdec.specdec_distill_backward(ctx, z, values, tokens, lse, saved, w, 1.0)
+    _check_distill(z[:2], values[:2], tokens[:2], lse[:2], 1.0, w[:2], dtype, loss[:2], grad[:2])
+    _check_distill(z[:2], values[:2], tokens[:2], lse[:2], 1.0, w[:2], dtype, loss1[:2], grad1[:2], weighted_loss=False)
+    _check_top(ctx, z[:2], 40, 1.0)
+    x = z[:2].view(1, 2, V) if z.is_contiguous() else z[:2].unsqueeze(0)
+    _check_beam(ctx, x, torch.tensor([[-1.0, -1.5]], device="cuda"), 5, 1.0)
+
+
 @pytest.mark.parametrize("dtype,V", [("f32", 150001), ("bf16", 270001)])
 def test_distill_of_rows_longer_than_a_clusters_registers(ctx, dtype, V):
     z, values, tokens, lse, w = _record(9, 3, V, 40, dtype, 1.0, True)
