@@ -22,8 +22,8 @@ namespace {
 using namespace rw;
 
 constexpr int MAX_TOP = SPECDEC_TOP_LOGITS_MAX;
-constexpr int CAP = 2048;                  // elements in the buffer
-constexpr int KEEP = 96;                   // vectors a warp can keep
+constexpr int CAP = 1536;                  // elements in the buffer
+constexpr int KEEP = 128;                  // vectors a warp can keep
 constexpr int PER_SM = 3;                  // CTAs of an SM; a fourth would leave 64 registers, and measured 10 % slower
 static_assert(MAX_TOP <= NT && CAP >= 2 * MAX_TOP && CAP % NT == 0, "the lists fit the buffer");
 static_assert(MAX_CLUSTER <= NW && MAX_TOP * 8 <= CHUNK * 16, "a warp for every list, with room for it");
@@ -166,21 +166,21 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
     constexpr int N = Row<T>::N;
     const Slice<T>& S = sh.S;
     const int lane = tid & 31, warp = tid >> 5;
-    const T* mine = reinterpret_cast<const T*>(sh.chunk[warp] + lane);       // element e of vector i: mine[i * 32 * N + e]
-    const int j0 = S.start(chunk) + lane;
-    auto value = [&](int i, int e) { return Row<T>::wide(mine[i * 32 * N + e]); };
+    const uint4* mine = sh.chunk[warp] + lane;      // vector i: mine[i * 32]
+    const int j0 = S.start(chunk) + lane, depth = has ? S.depth : 0;
     auto token = [&](int i, int e) { return (j0 + i * 32) * N - S.shift + e; };
-    auto is_real = [&](int i, int e) {
-        const int v = token(i, e);
-        return has && i < S.depth && j0 + i * 32 < S.v1 && v >= 0 && v < S.V;
-    };
+    auto is_real = [&](int i, int e) { return j0 + i * 32 < S.v1 && token(i, e) >= 0 && token(i, e) < S.V; };
     int turn = 0;
     // elements that are not below f; what lies past the row's ends is -inf
     auto count_from = [&](float f) {
         int n = 0;
 #pragma unroll 1
-        for (int i = 0; i < NV; ++i)
-            for (int e = 0; e < N; ++e) n += has && value(i, e) >= f ? 1 : 0;
+        for (int i = 0; i < depth; ++i) {
+            float x[N];
+            widen<T>(mine[i * 32], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) n += x[e] >= f ? 1 : 0;
+        }
         return block_count(n, sh.wcount[turn ^= 1], lane, warp);
     };
     // level: lo <= x < hi are the elements equal to the k-th largest, hi <= x those above it; `nans`: the level is NaN,
@@ -201,12 +201,15 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
     } else {
         int with_inf = 0, real = 0;
 #pragma unroll 1
-        for (int i = 0; i < NV; ++i)
-            for (int e = 0; e < N; ++e)
-                if (is_real(i, e)) {
-                    ++real;
-                    with_inf += value(i, e) >= lo ? 1 : 0;
-                }
+        for (int i = 0; i < depth; ++i) {
+            float x[N];
+            widen<T>(mine[i * 32], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                real += is_real(i, e) ? 1 : 0;
+                with_inf += is_real(i, e) && x[e] >= lo ? 1 : 0;
+            }
+        }
         with_inf = block_count(with_inf, sh.wcount[turn ^= 1], lane, warp);
         real = block_count(real, sh.wcount[turn ^= 1], lane, warp);
         need = min(need, real);
@@ -216,25 +219,30 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
         }
     }
     // above the level (2), on it (1)?
-    auto where = [&](int i, int e) {
-        if (!is_real(i, e)) return 0;
-        const float x = value(i, e);
-        return nans ? (x == x ? 2 : 1) : x >= hi ? 2 : x >= lo ? 1 : 0;
+    auto where = [&](float x, int i, int e) {
+        return !is_real(i, e) ? 0 : nans ? (x == x ? 2 : 1) : x >= hi ? 2 : x >= lo ? 1 : 0;
     };
     int ties = 0;
 #pragma unroll 1
-    for (int i = 0; i < NV; ++i)
-        for (int e = 0; e < N; ++e) ties += where(i, e) == 1 ? 1 : 0;
+    for (int i = 0; i < depth; ++i) {
+        float x[N];
+        widen<T>(mine[i * 32], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) ties += where(x[e], i, e) == 1 ? 1 : 0;
+    }
     block_count(ties, sh.wcount[turn ^= 1], lane, warp);
     int taken = above;                               // and the ties of the warps before: their tokens are lower
     for (int w = 0; w < warp; ++w) taken += sh.wcount[turn][w];
 #pragma unroll 1
-    for (int i = 0; i < NV; ++i) {                   // within a warp tokens grow with i, then with the lane, then with e
-        unsigned on = 0;
+    for (int i = 0; i < depth; ++i) {                // within a warp tokens grow with i, then with the lane, then with e
+        float x[N];
+        widen<T>(mine[i * 32], x);
+        unsigned on = 0, up = 0;
+#pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int w = where(i, e);
-            append(sh, w == 2, full_key(value(i, e), token(i, e)), lane);
-            if (w == 1) on |= 1u << e;
+            const int w = where(x[e], i, e);
+            on |= w == 1 ? 1u << e : 0u;
+            up |= w == 2 ? 1u << e : 0u;
         }
         const int own = __popc(on);
         int incl = own;
@@ -244,12 +252,14 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
             if (lane >= o) incl += t;
         }
         int before = taken + incl - own;
+        taken += __shfl_sync(0xffffffffu, incl, 31);
+        if (!__any_sync(0xffffffffu, up != 0 || (on != 0 && before < need))) continue;
+#pragma unroll
         for (int e = 0; e < N; ++e) {
             const bool tie = (on >> e) & 1u;
-            append(sh, tie && before < need, full_key(value(i, e), token(i, e)), lane);
+            append(sh, ((up >> e) & 1u) || (tie && before < need), full_key(x[e], token(i, e)), lane);
             before += tie ? 1 : 0;
         }
-        taken += __shfl_sync(0xffffffffu, incl, 31);
     }
 }
 
@@ -271,15 +281,37 @@ __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
     for (int step = 0; step < steps; ++step) {
         const int chunk = S.first_chunk(warp) + step, j0 = S.start(chunk);
         const bool has = step < S.chunks_of(warp);
-        chunk_wait();
         if (has) S.fetch(j0, lane, sh.chunk[warp]);
         chunk_wait();
-        const T* mine = reinterpret_cast<const T*>(sh.chunk[warp] + lane);
+        const uint4* mine = sh.chunk[warp] + lane;
+        const int depth = has ? S.depth : 0;
+        if (step == 0) {                            // k of the thread maxima reach the k-th largest of them
+            float m = -INFINITY;
+            for (int i = 0; i < depth; ++i) {
+                const float x = Max<T>{mine[i * 32]}.value();
+                m = fmaxf(m, x);
+            }
+            sh.tmax[tid] = m;
+            __syncthreads();
+            if (warp == 0) {
+                const float b = rth_of_maxima(sh.tmax, k, lane);
+                if (lane == 0) sh.first_bound = b;
+            }
+            __syncthreads();
+            least = sh.first_bound;
+        }
 #pragma unroll 1
-        for (int q = 0; q < NV * N; ++q) {
-            const int i = q / N, e = q % N, j = j0 + i * 32 + lane, v = j * N - S.shift + e;
-            const float x = Row<T>::wide(mine[i * 32 * N + e]);
-            append(sh, has && i < S.depth && j < S.v1 && v >= 0 && v < S.V && !(x < least || (x == least && v >= least_token)), full_key(x, v), lane);
+        for (int i = 0; i < depth; ++i) {
+            const uint4 r = mine[i * 32];
+            if (!__any_sync(0xffffffffu, !(Max<T>{r}.value() < least))) continue;
+            const int j = j0 + i * 32 + lane;
+            float x[N];
+            widen<T>(r, x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int v = j * N - S.shift + e;
+                append(sh, j < S.v1 && v >= 0 && v < S.V && !(x[e] < least || (x[e] == least && v >= least_token)), full_key(x[e], v), lane);
+            }
         }
         __syncthreads();
         int n = sh.count;
