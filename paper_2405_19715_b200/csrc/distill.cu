@@ -14,8 +14,8 @@
 // the list, and the difference would keep few digits.  A bitmap of the CTA's part of the row tells list from rest.
 // sum p, R and the loss are in 64 bits for the same reason; they are a few values per listed token.
 //
-// The 8 warps of a CTA have a stretch of the row each, and go through it in chunks of 4 KB, the next one on its way into
-// shared memory meanwhile: once for the terms' sums, and a step goes back over it, from the chunk that is still in
+// The 8 warps of a CTA go through their share of the row in chunks of 4 KB, the next one on its way into shared memory
+// meanwhile: once for the terms' sums, and a step goes back over it, from the chunk that is still in
 // registers, for the gradient.  Rows are cut over the CTAs of a cluster until those that are worked on at one time fit L2
 // twice over, so that the way back reads no memory: one read and one write of the row.  Sums meet through distributed
 // shared memory, one record a warp.  A listed token belongs to the CTA that has its logit, which adds its part to the
@@ -75,19 +75,6 @@ __device__ __forceinline__ unsigned listed_bits(const uint32_t* bitmap, int j) {
     return Row<T>::N == 8 ? bytes[j] : bytes[j >> 1] >> (4 * (j & 1)) & 15u;
 }
 
-// The same for logits so large that only those equal to the largest count; from memory, rarely.
-template <typename T>
-__device__ __noinline__ void huge_terms(const Slice<T>& S, const uint32_t* bitmap, int j0, float top, int lane, float& s_out, float& s_in) {
-#pragma unroll 1
-    for (int i = 0; i < S.depth; ++i)
-        for (int e = 0; e < Row<T>::N; ++e) {
-            const int j = j0 + i * 32 + lane, v = j * Row<T>::N - S.shift + e;
-            if (j >= S.v1 || v < 0 || v >= S.V) continue;
-            const float t = top == INFINITY ? NAN : huge_term(Row<T>::wide(S.row[v]), top);
-            if (listed_bits<T>(bitmap, j - S.v0) >> e & 1u) s_in += t; else s_out += t;
-        }
-}
-
 template <typename T, DistillMode MODE>
 __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill_kernel(const __grid_constant__ DistillParams P) {
     constexpr int N = Row<T>::N;
@@ -111,8 +98,8 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
     // asked for before anything is computed
     const int first_id = list0 < k ? tokens[list0] : -1;
     const float first_v = list0 < k ? values[list0] : 0.f, lse = P.lse ? P.lse[row_id] : 0.f;
-    const Slice<T> S(static_cast<const T*>(P.z) + row_id * P.z_stride, P.V, C, rank);
-    const int own_steps = S.chunks_of(warp), stride = 32 * S.depth, j_first = S.start(S.first_chunk(warp));
+    const Slice<T, false> S(static_cast<const T*>(P.z) + row_id * P.z_stride, P.V, C, rank);
+    const int own_steps = S.steps_of(warp), j_first = S.start(0, warp);
     const float weight = GRAD ? P.weight[row_id] : 1.f;
 
     T* grad = GRAD ? static_cast<T*>(P.grad) + row_id * P.g_stride : nullptr;
@@ -182,7 +169,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
     float s_out = 0.f, s_in = 0.f, top = -INFINITY;              // this lane's terms outside and inside the list
     if (STATS && !zero) {
         int j0 = j_first;
-        for (int step = 0; step < own_steps; ++step, j0 += stride) {
+        for (int step = 0; step < own_steps; ++step, j0 += CHUNK) {
             chunk_wait();
 #pragma unroll
             for (int i = 0; i < NV; ++i) r[i] = sh.chunk[warp][i * 32 + lane];
@@ -191,8 +178,8 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
             for (int i = 1; i < NV; ++i) mx = Max<T>{mx, Max<T>{r[i]}};
             const float own = mx.value(), wm = warp_max(own == own ? own : -INFINITY);    // NaN is met in the sums
             // the next chunk, or the one before, with which the way back begins: this one stays in registers
-            if (step + 1 < own_steps) S.fetch(j0 + stride, lane, sh.chunk[warp], TWICE);
-            else if (GRAD && step > 0 && straight && S.whole(j0)) S.fetch(j0 - stride, lane, sh.chunk[warp]);
+            if (step + 1 < own_steps) S.fetch(j0 + CHUNK, lane, sh.chunk[warp], TWICE);
+            else if (GRAD && step > 0 && straight && S.whole(j0)) S.fetch(j0 - CHUNK, lane, sh.chunk[warp]);
             if (wm > top) {
                 const float f = move_terms(top, wm, P.c);        // the sums are 0 so far where top is -inf
                 s_out *= f;
@@ -208,7 +195,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                 for (int i = 0; i < NV; ++i) {
                     f2 x[N / 2];
                     pairs(r[i], x, T());
-                    const unsigned bits = listed_bits<T>(bitmap, j0 - S.v0 + lane + i * 32);      // what is no vector has terms of 0
+                    const unsigned bits = listed_bits<T>(bitmap, j0 - S.v0 + lane + i * S.apart());      // what is no vector has terms of 0
                     f2 e[N / 2];
 #pragma unroll
                     for (int q = 0; q < N / 2; ++q) e[q] = term2(x[q], c2, neg);
@@ -228,7 +215,17 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                 s_out += fold2(acc);
                 s_in += in;
             } else {
-                huge_terms(S, bitmap, j0, top, lane, s_out, s_in);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const unsigned bits = listed_bits<T>(bitmap, j0 - S.v0 + lane + i * S.apart());
+                    float x[N];
+                    widen<T>(opaque(r[i]), x);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float y = huge_term(x[e], top);
+                        if (bits >> e & 1u) s_in += y; else s_out += y;
+                    }
+                }
             }
         }
     }
@@ -354,8 +351,8 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
         const float u = m * P.c;
         const f2 c2 = sd::pack2(P.c, P.c), neg = sd::pack2(-u, -u), scale2 = sd::pack2(scale, scale);
         const bool plain = ordinary(m) && !zero;
-        const int back = STATS ? -stride : stride;
-        int j0 = STATS ? j_first + (own_steps - 1) * stride : j_first;
+        const int back = STATS ? -CHUNK : CHUNK;
+        int j0 = STATS ? j_first + (own_steps - 1) * CHUNK : j_first;
         for (int n = 0; n < own_steps; ++n, j0 += back) {
             const bool in_registers = STATS && n == 0;
             if (!in_registers) chunk_wait();
@@ -381,8 +378,8 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
             // another alignment than the logits': that goes back through shared memory, to be stored element next to element
             T* const staged = reinterpret_cast<T*>(sh.chunk[warp]);
 #pragma unroll 1
-            for (int i = 0; i < S.depth; ++i) {
-                const int j = j0 + i * 32 + lane, e0 = j * N - S.shift;
+            for (int i = 0; i < NV; ++i) {
+                const int j = j0 + i * S.apart() + lane, e0 = j * N - S.shift;
                 if (j >= S.v1) break;
                 float g[N];
                 widen<T>(sh.chunk[warp][i * 32 + lane], g);
@@ -401,9 +398,12 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
             }
             if (!straight) {
                 __syncwarp();
-                const int e0 = j0 * N - S.shift, end = min(stride, S.v1 - j0) * N;
-                for (int e = lane; e < end; e += 32)
-                    if (e0 + e >= 0 && e0 + e < S.V) grad[e0 + e] = staged[e];
+#pragma unroll 1
+                for (int i = 0; i < NV; ++i) {      // piece by piece
+                    const int j = j0 + i * S.apart(), e0 = j * N - S.shift, end = min(32, S.v1 - j) * N;
+                    for (int e = lane; e < end; e += 32)
+                        if (e0 + e >= 0 && e0 + e < S.V) grad[e0 + e] = staged[i * 32 * N + e];
+                }
                 __syncwarp();
             }
             if (!zero && n + 1 < own_steps) S.fetch(j0 + back, lane, sh.chunk[warp]);
@@ -447,9 +447,11 @@ cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mod
         while (least < MAX_CLUSTER && std::min<long long>(rows, 3ll * sm_count / least) * most * 16 > (80ll << 20)) least *= 2;
     // the bitmap of a CTA's part takes at most 128 KB of shared memory
     if (mode != DistillMode::Gradient)
-        while (least < MAX_CLUSTER && (most / least + CHUNK) * n > (128 << 13)) least *= 2;
+        while (least < MAX_CLUSTER && most / least * n > (128 << 13)) least *= 2;
     p.cluster = rw::cluster_size(rows, most, 2 * sm_count, least);
-    p.slice_words = mode == DistillMode::Gradient ? 0 : (((most + p.cluster - 1) / p.cluster + CHUNK) * n + 31) / 32;      // whole chunks
+    // whole pieces, eight times as many as an eighth of the part has: a lane looks up vectors that are not there, too
+    const int chunks = (((most + p.cluster - 1) / p.cluster + 31) / 32 + NV - 1) / NV;
+    p.slice_words = mode == DistillMode::Gradient ? 0 : chunks * NV * n;
     const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 20;
     if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, smem, s);
     if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, smem, s);

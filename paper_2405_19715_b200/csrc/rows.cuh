@@ -145,14 +145,18 @@ __device__ __forceinline__ uint4 edge_vector(const T* row, int e0, int V) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A CTA's part of a row, [v0, v1) of its vectors, in chunks that a warp holds at a time: 32 * depth vectors, 8 of them a
-// lane (4 KB) unless the part is too short to give every warp such a chunk.  Every warp has a range of chunks that follow
-// one another.  Vectors [in0, in0 + in_n) lie inside the row.
+// A CTA's part of a row, [v0, v1) of its vectors, in chunks that a warp holds at a time: 8 pieces of 32 vectors (4 KB).
+// Vectors [in0, in0 + in_n) lie inside the row.
+//   Not spread: a chunk's pieces follow one another, and a warp's chunks do.
+//   Spread: piece i is one of the part's i-th eighth, and which one goes through the eighth along a diagonal over warps and
+//   steps.  The warps' first chunks are then a sample of the whole part, and what lies close together in a row (vocabularies
+//   have their frequent tokens in front) is dealt out to all warps.  Reading 512 bytes here and there costs 3 to 10 %.
 constexpr int CHUNK = 32 * NV;
-template <typename T>
+template <typename T, bool SPREAD>
 struct Slice {
     const T* row;
-    int shift, V, v0, v1, in0, in_n, depth, base, extra;
+    int shift, V, v0, v1, in0, in_n;
+    int chunks, block;                             // how many; spread: pieces of an eighth, and of an eighth of that
     __device__ __forceinline__ Slice(const T* row_, int V_, int C, int rank) {
         row = row_;
         V = V_;
@@ -162,21 +166,25 @@ struct Slice {
         v1 = min(nvec, v0 + per);
         in0 = max(v0, shift ? 1 : 0);
         in_n = max(0, min(v1, (shift + V) / Row<T>::N) - in0);
-        depth = min(NV, max(1, (v1 - v0 + NT - 1) / NT));
-        const int chunks = (v1 - v0 + 32 * depth - 1) / (32 * depth);
-        base = chunks / NW;                        // every warp has that many, the first `extra` one more
-        extra = chunks % NW;
+        chunks = ((v1 - v0 + 31) / 32 + NV - 1) / NV;
+        block = (chunks + NW - 1) / NW;
     }
-    __device__ __forceinline__ int first_chunk(int warp) const { return warp * base + min(warp, extra); }
-    __device__ __forceinline__ int chunks_of(int warp) const { return base + (warp < extra ? 1 : 0); }
-    __device__ __forceinline__ int steps() const { return base + (extra ? 1 : 0); }      // of the warp that has most
-    __device__ __forceinline__ int start(int chunk) const { return v0 + chunk * 32 * depth; }
+    __device__ __forceinline__ int apart() const { return SPREAD ? chunks * 32 : 32; }       // vectors from one piece to the next
+    // steps of a warp; where the part is spread some may have no chunk
+    __device__ __forceinline__ int steps() const { return block; }
+    __device__ __forceinline__ int steps_of(int warp) const { return SPREAD ? block : (chunks + NW - 1 - warp) / NW; }
+    // first vector of a warp's chunk; v1 or more: none
+    __device__ __forceinline__ int start(int step, int warp) const {
+        if (!SPREAD) return v0 + (warp * (chunks / NW) + min(warp, chunks % NW) + step) * CHUNK;
+        const int at = (warp + step) % NW * block + step;
+        return at < chunks && step < block ? v0 + at * 32 : 0x7ffffff0;
+    }
     // whether all of the chunk that starts at vector j0 lies inside the row
-    __device__ __forceinline__ bool whole(int j0) const { return depth == NV && j0 >= in0 && j0 + CHUNK <= in0 + in_n; }
+    __device__ __forceinline__ bool whole(int j0) const { return j0 >= in0 && j0 + (NV - 1) * apart() + 32 <= in0 + in_n; }
     __device__ __forceinline__ bool inside(int j) const { return (unsigned)(j - in0) < (unsigned)in_n; }
     __device__ __forceinline__ const T* address(int j) const { return row + ((long long)j * Row<T>::N - shift); }
     // The copy into shared memory of the chunk that starts at vector j0, asynchronous: it costs no register while it is on
-    // its way.  A lane reads back, after chunk_wait(), only what it has asked for itself: vector j0 + i * 32 + lane at
+    // its way.  A lane reads back, after chunk_wait(), only what it has asked for itself: vector j0 + i * apart() + lane at
     // buffer[i * 32 + lane].  -inf where there is no vector.  `again`: the chunk will be read once more, and should stay
     // in L2 meanwhile; otherwise it is the first to go.
     __device__ __forceinline__ void fetch(int j0, int lane, uint4* buffer, bool again = false) const {
@@ -186,16 +194,16 @@ struct Slice {
         const unsigned long long policy = again ? normal : first;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(buffer + lane);
         if (whole(j0)) {
-            const T* p = address(j0 + lane);
+            const char* p = reinterpret_cast<const char*>(address(j0 + lane));
+            const long long step = (long long)apart() * 16;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + i * 512), "l"(p + i * 32 * Row<T>::N), "l"(policy)
-                             : "memory");
+            for (int i = 0; i < NV; ++i, p += step)
+                asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + i * 512), "l"(p), "l"(policy) : "memory");
         } else {
             const uint32_t w = Row<T>::neg_inf();
 #pragma unroll 1
             for (int i = 0; i < NV; ++i) {
-                const int j = i < depth ? j0 + i * 32 + lane : v1;
+                const int j = j0 + i * apart() + lane;
                 if (inside(j)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(address(j)) : "memory");
                 else buffer[i * 32 + lane] = j < v1 ? edge_vector<T>(row, j * Row<T>::N - shift, V) : make_uint4(w, w, w, w);
             }
@@ -225,7 +233,12 @@ __device__ __forceinline__ float fold2(f2 a) {
 // there two values are equal or too far apart for the smaller one to count.
 constexpr float HUGE_LOGIT = 1.0e30f;
 __device__ __forceinline__ bool ordinary(float m) { return m <= HUGE_LOGIT && m >= -HUGE_LOGIT; }
-__device__ __forceinline__ float huge_term(float x, float m) { return x == m ? 1.f : x == x ? 0.f : x; }
+__device__ __forceinline__ float huge_term(float x, float m) { return m == INFINITY ? NAN : x == m ? 1.f : x == x ? 0.f : x; }
+// Keeps the compiler from widening a vector once for both this case and the ordinary one, and holding on to all of it.
+__device__ __forceinline__ uint4 opaque(uint4 r) {
+    asm volatile("" : "+r"(r.x), "+r"(r.y), "+r"(r.z), "+r"(r.w));
+    return r;
+}
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -1,8 +1,8 @@
 // The k largest logits of a row in order, and the row's log-sum-exp: what a draft model's training keeps of a target
 // row, and what beam selection starts from.
 //
-// The row passes through registers once.  The 8 warps of a CTA have a stretch of it each, and go through it by themselves
-// in chunks of 4 KB, the next one on its way into shared memory meanwhile.
+// The row passes through registers once.  The 8 warps of a CTA go through their share of it by themselves, in chunks of 4 KB,
+// the next one on its way into shared memory meanwhile.
 //   The bound.  The r-th largest of the 256 thread maxima of the warps' first chunks, which are a sample of the row, with
 //     r the number of the k largest that such a sample should hold and 2.5 standard deviations more: about k and half as
 //     many of the row's elements reach it.
@@ -31,7 +31,7 @@ static_assert(MAX_CLUSTER <= NW && MAX_TOP * 8 <= CHUNK * 16, "a warp for every 
 // Everything that all threads share lives here, the row's geometry among it: the registers of a thread hold its vectors.
 template <typename T>
 struct TopShared {
-    Slice<T> S;
+    Slice<T, true> S;
     uint4 chunk[NW][CHUNK];                // each warp's coming chunk; at the end the list of another CTA
     union {
         uint4 vec[NW][KEEP];
@@ -48,28 +48,32 @@ struct TopShared {
     Part part, whole;                      // of the CTA, of the cluster
 };
 
-// The r-th largest of the 256 thread maxima, or a value just below it (its key's leading 16 bits); -inf if fewer are
-// above -inf.  One warp; r <= NT.
+// The r-th largest of the 256 thread maxima, or the least of those that share the 16 leading bits of its key.  One warp;
+// r <= NT.
 __device__ __forceinline__ float rth_of_maxima(const float (&tmax)[NT], int r, int lane) {
-    uint32_t key[NT / 32];
+    uint32_t key[NT / 32], least = 0xffffffffu, most = 0;
 #pragma unroll
-    for (int i = 0; i < NT / 32; ++i) key[i] = value_key(tmax[i * 32 + lane]) >> 16;
-    uint32_t least = key[0], most = key[0];
-#pragma unroll
-    for (int i = 1; i < NT / 32; ++i) { least = min(least, key[i]); most = max(most, key[i]); }
+    for (int i = 0; i < NT / 32; ++i) {
+        key[i] = value_key(tmax[i * 32 + lane]);
+        least = min(least, key[i]);
+        most = max(most, key[i]);
+    }
     least = __reduce_min_sync(0xffffffffu, least);
     most = __reduce_max_sync(0xffffffffu, most);
-    const int bits = 32 - __clz(least ^ most);       // the leading bits are those of all of them
-    uint32_t prefix = most >> bits << bits;
+    const int bits = 32 - __clz((least ^ most) | 0xffffu);       // the leading bits are those of all of them
+    uint32_t prefix = bits < 32 ? most >> bits << bits : 0u;
 #pragma unroll 1
-    for (int bit = bits - 1; bit >= 0; --bit) {
+    for (int bit = bits - 1; bit >= 16; --bit) {
         const uint32_t trial = prefix | (1u << bit);
         int c = 0;
 #pragma unroll
         for (int i = 0; i < NT / 32; ++i) c += key[i] >= trial ? 1 : 0;
         if ((int)__reduce_add_sync(0xffffffffu, c) >= r) prefix = trial;
     }
-    return prefix > 0x007f ? key_value(prefix << 16) : -INFINITY;
+    uint32_t exact = 0xffffffffu;                    // a value that there is: ties with it are found as such
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) exact = key[i] >= prefix ? min(exact, key[i]) : exact;
+    return key_value(__reduce_min_sync(0xffffffffu, exact));
 }
 
 // Sum of one int per thread over the CTA; `buf` alternates between two sets so that one barrier is enough.
@@ -162,14 +166,14 @@ __device__ __forceinline__ void append(TopShared<T>& sh, bool has, unsigned long
 // the chunks in shared memory: the value of the k-th largest is built from its key's leading bits; elements above it are
 // all taken, those equal to it in token order.
 template <typename T>
-__device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has, int k, int tid) {
+__device__ __forceinline__ void count_over(TopShared<T>& sh, int step, bool has, int k, int tid) {
     constexpr int N = Row<T>::N;
-    const Slice<T>& S = sh.S;
+    const Slice<T, true>& S = sh.S;
     const int lane = tid & 31, warp = tid >> 5;
     const uint4* mine = sh.chunk[warp] + lane;      // vector i: mine[i * 32]
-    const int j0 = S.start(chunk) + lane, depth = has ? S.depth : 0;
-    auto token = [&](int i, int e) { return (j0 + i * 32) * N - S.shift + e; };
-    auto is_real = [&](int i, int e) { return j0 + i * 32 < S.v1 && token(i, e) >= 0 && token(i, e) < S.V; };
+    const int j0 = S.start(step, warp) + lane, depth = has ? NV : 0;
+    auto token = [&](int i, int e) { return (j0 + i * S.apart()) * N - S.shift + e; };
+    auto is_real = [&](int i, int e) { return j0 + i * S.apart() < S.v1 && token(i, e) >= 0 && token(i, e) < S.V; };
     int turn = 0;
     // elements that are not below f; what lies past the row's ends is -inf
     auto count_from = [&](float f) {
@@ -222,25 +226,15 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
     auto where = [&](float x, int i, int e) {
         return !is_real(i, e) ? 0 : nans ? (x == x ? 2 : 1) : x >= hi ? 2 : x >= lo ? 1 : 0;
     };
-    int ties = 0;
+    int taken = above;                               // ties still wanted: need - taken
 #pragma unroll 1
-    for (int i = 0; i < depth; ++i) {
-        float x[N];
-        widen<T>(mine[i * 32], x);
-#pragma unroll
-        for (int e = 0; e < N; ++e) ties += where(x[e], i, e) == 1 ? 1 : 0;
-    }
-    block_count(ties, sh.wcount[turn ^= 1], lane, warp);
-    int taken = above;                               // and the ties of the warps before: their tokens are lower
-    for (int w = 0; w < warp; ++w) taken += sh.wcount[turn][w];
-#pragma unroll 1
-    for (int i = 0; i < depth; ++i) {                // within a warp tokens grow with i, then with the lane, then with e
+    for (int i = 0; i < NV; ++i) {                   // tokens grow with i, then with the warps' order in this step, the lane, e
         float x[N];
         widen<T>(mine[i * 32], x);
         unsigned on = 0, up = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int w = where(x[e], i, e);
+            const int w = has ? where(x[e], i, e) : 0;
             on |= w == 1 ? 1u << e : 0u;
             up |= w == 2 ? 1u << e : 0u;
         }
@@ -251,8 +245,11 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
             const int t = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += t;
         }
+        const int all = block_count(own, sh.wcount[turn ^= 1], lane, warp);
         int before = taken + incl - own;
-        taken += __shfl_sync(0xffffffffu, incl, 31);
+        for (int w = 0; w < NW; ++w)
+            if (S.start(step, w) < S.start(step, warp)) before += sh.wcount[turn][w];
+        taken += all;
         if (!__any_sync(0xffffffffu, up != 0 || (on != 0 && before < need))) continue;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -269,7 +266,7 @@ __device__ __forceinline__ void count_over(TopShared<T>& sh, int chunk, bool has
 template <typename T>
 __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
     constexpr int N = Row<T>::N;
-    const Slice<T>& S = sh.S;
+    const Slice<T, true>& S = sh.S;
     const int lane = tid & 31, warp = tid >> 5, steps = S.steps();
     __syncthreads();
     if (tid == 0) sh.count = sh.n_list = 0;
@@ -279,12 +276,12 @@ __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
     int least_token = 0x7fffffff;
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
-        const int chunk = S.first_chunk(warp) + step, j0 = S.start(chunk);
-        const bool has = step < S.chunks_of(warp);
+        const int j0 = S.start(step, warp);
+        const bool has = j0 < S.v1;
         if (has) S.fetch(j0, lane, sh.chunk[warp]);
         chunk_wait();
         const uint4* mine = sh.chunk[warp] + lane;
-        const int depth = has ? S.depth : 0;
+        const int depth = has ? NV : 0;
         if (step == 0) {                            // k of the thread maxima reach the k-th largest of them
             float m = -INFINITY;
             for (int i = 0; i < depth; ++i) {
@@ -304,7 +301,7 @@ __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
         for (int i = 0; i < depth; ++i) {
             const uint4 r = mine[i * 32];
             if (!__any_sync(0xffffffffu, !(Max<T>{r}.value() < least))) continue;
-            const int j = j0 + i * 32 + lane;
+            const int j = j0 + i * S.apart() + lane;
             float x[N];
             widen<T>(r, x);
 #pragma unroll
@@ -319,7 +316,7 @@ __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
         if (n > CAP) {
             if (tid == 0) sh.count = sh.n_list;     // the list is at the front of the buffer: nothing else was in it
             __syncthreads();
-            count_over(sh, chunk, has, k, tid);
+            count_over(sh, step, has, k, tid);
             __syncthreads();
             n = sh.count;
             __syncthreads();
@@ -336,25 +333,11 @@ __device__ __noinline__ void careful_pass(TopShared<T>& sh, int k, int tid) {
     }
 }
 
-// This thread's terms of a chunk against a value so large that only equal ones count; from memory, rarely.
-template <typename T>
-__device__ __noinline__ float huge_terms(const TopShared<T>& sh, int j0, float top, int lane) {
-    const Slice<T>& S = sh.S;
-    float s = top == INFINITY ? NAN : 0.f;
-#pragma unroll 1
-    for (int i = 0; i < S.depth; ++i)
-        for (int e = 0; e < Row<T>::N; ++e) {
-            const int j = j0 + i * 32 + lane, v = j * Row<T>::N - S.shift + e;
-            if (j < S.v1 && v >= 0 && v < S.V) s += huge_term(Row<T>::wide(S.row[v]), top);
-        }
-    return s;
-}
-
 // Elements equal to x, in token order, until the buffer holds k: what is left of a list when nothing else comes before
 // them.  Called by the whole CTA.
 template <typename T>
 __device__ __noinline__ void fill_with(TopShared<T>& sh, float x, int k, int tid) {
-    const Slice<T>& S = sh.S;
+    const Slice<T, true>& S = sh.S;
     const int lane = tid & 31, warp = tid >> 5, e0 = max(0, S.v0 * Row<T>::N - S.shift), e1 = min(S.V, S.v1 * Row<T>::N - S.shift);
     int turn = 0, n = sh.count;
 #pragma unroll 1
@@ -386,7 +369,7 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
     }
     if (tid == 0) {
         const int outer = row_id / P.inner, in = row_id - outer * P.inner;
-        sh.S = Slice<T>(static_cast<const T*>(P.x) + outer * P.outer_stride + in * P.row_stride, P.V, P.cluster, blockIdx.x - row_id * P.cluster);
+        sh.S = Slice<T, true>(static_cast<const T*>(P.x) + outer * P.outer_stride + in * P.row_stride, P.V, P.cluster, blockIdx.x - row_id * P.cluster);
         sh.count = sh.n_list = 0;
     }
     __syncthreads();
@@ -394,9 +377,9 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
     double sum = 0.0;                               // of this thread's terms, against its warp's largest value
     float top = -INFINITY;
     {
-        const Slice<T>& S = sh.S;
+        const Slice<T, true>& S = sh.S;
         // how many of the k largest the first chunks should hold, and some more
-        const int steps = S.steps(), own_steps = S.chunks_of(warp), stride = 32 * S.depth;
+        const int steps = S.steps();
         const float share = (float)P.k / (float)max(steps, 1);
         int want = steps > 1 ? min(P.k, (int)(share + 3.5f * sqrtf(share)) + 2) : P.k;
         const int real = min(S.V, S.v1 * N - S.shift) - max(0, S.v0 * N - S.shift);
@@ -405,9 +388,11 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
         for (int attempt = 0;; ++attempt) {
             float bound = above;
             int kept = 0;                               // vectors of this warp that reach the bound
-            int j0 = S.start(S.first_chunk(warp));
-            if (own_steps > 0) S.fetch(j0, lane, sh.chunk[warp]);
-            for (int step = 0; step == 0 || step < own_steps; ++step, j0 += stride) {
+            int j0 = S.start(0, warp);
+            if (j0 < S.v1) S.fetch(j0, lane, sh.chunk[warp]);
+            for (int step = 0; step == 0 || step < steps; ++step) {
+                const bool has = j0 < S.v1;
+                const int next = S.start(step + 1, warp);
                 chunk_wait();
                 uint4 r[NV];
 #pragma unroll
@@ -415,7 +400,7 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                 Max<T> mx{r[0]};
 #pragma unroll
                 for (int i = 1; i < NV; ++i) mx = Max<T>{mx, Max<T>{r[i]}};
-                const float m = own_steps > 0 ? mx.value() : -INFINITY;
+                const float m = has ? mx.value() : -INFINITY;
                 if (step == 0) {
                     sh.tmax[tid] = m == m ? m : -INFINITY;
                     __syncthreads();
@@ -424,8 +409,8 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                         if (lane == 0) sh.first_bound = b;
                     }
                 }
-                if (step + 1 < own_steps) S.fetch(j0 + stride, lane, sh.chunk[warp]);        // this one is in registers
-                if (own_steps > 0 && attempt == 0) {
+                if (next < S.v1) S.fetch(next, lane, sh.chunk[warp]);        // this one is in registers
+                if (has && attempt == 0) {
                     const float wm = warp_max(m == m ? m : -INFINITY);
                     if (wm > top) {
                         sum *= (double)move_terms(top, wm, P.c);         // 0 so far where top is -inf
@@ -443,7 +428,15 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                         }
                         sum += (double)fold2(acc);
                     } else {
-                        sum += (double)huge_terms(sh, j0, top, lane);
+                        float acc = 0.f;
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            float x[N];
+                            widen<T>(opaque(r[i]), x);
+#pragma unroll
+                            for (int e = 0; e < N; ++e) acc += huge_term(x[e], top);
+                        }
+                        sum += (double)acc;
                     }
                 }
                 if (step == 0) {
@@ -464,12 +457,13 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                             const int at = kept + __popc(who & ((1u << lane) - 1u));
                             if (on && at < KEEP) {
                                 sh.vec[warp][at] = r[i];
-                                sh.vec_at[warp][at] = j0 + i * 32 + lane;
+                                sh.vec_at[warp][at] = j0 + i * S.apart() + lane;
                             }
                             kept += __popc(who);
                         }
                     }
                 }
+                j0 = next;
             }
             // ---- the list.  NaN, which ranks last, is left to the careful pass
             __syncwarp();
