@@ -390,7 +390,8 @@ int specdec_verify_correct_static(const void* target_logits, const void* draft_l
  *
  * They take rows of V logits, f32, bf16 or f16, whose elements follow one another; rows may lie at any stride >= V
  * and any alignment of whole elements.  Nothing outside a row's V elements is read or written.  Sizes do not depend on
- * max_B and max_K of the context, which owns no buffer of these calls: calls on several streams may overlap.
+ * max_B and max_K of the context, which owns no buffer of these calls: calls on several streams may overlap.  As with
+ * every call of a context, one host thread at a time makes them.
  * V <= 2^22; temperature T in [2^-20, 2^20].  The same call on rows of the same alignment gives the same
  * bits every time.
  */
@@ -400,7 +401,8 @@ int specdec_verify_correct_static(const void* target_logits, const void* draft_l
  *   values  dev out [rows, top_k] f32    descending; equal logits in the order of their tokens; NaN ranks below -inf
  *   tokens  dev out [rows, top_k] int32  their tokens
  *   lse     dev out [rows] f32 or NULL   log sum_v exp(logit_v / T): -inf for a row without a logit above -inf,
- *                                        NaN for a row with NaN or +inf
+ *                                        NaN for a row with NaN or +inf; infinite where the value itself is beyond
+ *                                        f32 (logits / T of 2^128), which is then of no use to what reads it
  * 1 <= top_k <= min(V, SPECDEC_TOP_LOGITS_MAX).  Terms are summed in fp32 within a thread, in 64 bits beyond it.
  * Errors: EINVAL (null pointer, extents, stride < V, temperature, dtype, top_k), EUNSUPPORTED (V > 2^22), ECUDA.
  */

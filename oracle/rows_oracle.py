@@ -32,6 +32,13 @@ def top_logits(z, k, T):
     return np.take_along_axis(z, order, -1), order.astype(np.int32), log_sum_exp(z, T)
 
 
+def listed_mass(v, lse, T):
+    """p of the listed logits v: against the target's log-sum-exp, or renormalised over the list where that is None."""
+    with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
+        log_p = v / T - float(lse) if lse is not None else v if np.isneginf(v).all() else log_softmax(v, T)
+        return np.where(np.isneginf(v), 0.0, np.exp(log_p))
+
+
 def distill_row(z, values, tokens, lse, T, weight=1.0):
     """(loss, gradient * weight) of one row; lse None: renormalised over the list.  Gradient [V]."""
     z = np.asarray(z, np.float64)
@@ -42,9 +49,8 @@ def distill_row(z, values, tokens, lse, T, weight=1.0):
         return np.nan, np.zeros(V)
     if len(y) == 0:
         return 0.0, np.zeros(V)
-    norm = float(lse) if lse is not None else log_sum_exp(v, T)
     with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
-        p = np.where(np.isneginf(v), 0.0, np.exp(v / T - norm))
+        p = listed_mass(v, lse, T)
         if np.isneginf(z).all():
             return (np.inf if (p > 0).any() else 0.0), np.zeros(V)
         log_q = log_softmax(z, T)

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                 s_in *= f;
                 top = wm;
             }
-            if (ordinary(top) || top == -INFINITY) {
+            if (ordinary(top * P.c) || top == -INFINITY) {
                 const float u = reference(top) * P.c;
                 const f2 neg = sd::pack2(-u, -u), c2 = sd::pack2(P.c, P.c);
                 f2 acc = sd::pack2(0.f, 0.f);
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
         // ---- the gradient: a step goes back from the chunk that the registers hold
         const float u = m * P.c;
         const f2 c2 = sd::pack2(P.c, P.c), neg = sd::pack2(-u, -u), scale2 = sd::pack2(scale, scale);
-        const bool plain = ordinary(m) && !zero;
+        const bool plain = ordinary(u) && !zero;
         const int back = STATS ? -CHUNK : CHUNK;
         int j0 = STATS ? j_first + (own_steps - 1) * CHUNK : j_first;
         for (int n = 0; n < own_steps; ++n, j0 += back) {
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
                 widen<T>(sh.chunk[warp][i * 32 + lane], g);
 #pragma unroll
                 for (int e = 0; e < N; ++e)
-                    g[e] = zero ? 0.f : (ordinary(m) ? sd::ex2(fmaf(g[e], P.c, -u)) : huge_term(g[e], m)) * scale;
+                    g[e] = zero ? 0.f : (ordinary(u) ? sd::ex2(fmaf(g[e], P.c, -u)) : huge_term(g[e], m)) * scale;
                 if (straight && e0 >= 0 && e0 + N <= S.V) {
                     store_vec<T>(grad + e0, g);
                 } else {
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
             __syncthreads();                        // the CTA's part is written: the listed tokens are written over
             for (int i = list0; i < k; i += NT)
                 if (const int id = ids[i]; id >= 0) {
-                    const float q = (ordinary(m) ? sd::ex2(fmaf(zs[i], P.c, -u)) : huge_term(zs[i], m)) * inv_s;
+                    const float q = (ordinary(u) ? sd::ex2(fmaf(zs[i], P.c, -u)) : huge_term(zs[i], m)) * inv_s;
                     store_one(grad + id, (float)(wt * (mass * (double)q - prob[i] / e_sum)));
                 }
         }

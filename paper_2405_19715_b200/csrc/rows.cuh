@@ -229,10 +229,10 @@ __device__ __forceinline__ float fold2(f2 a) {
     sd::unpack2(a, x, y);
     return x + y;
 }
-// Logits so large that x*c could overflow (rows masked with the type's lowest value) do not go through a multiply-add:
-// there two values are equal or too far apart for the smaller one to count.
-constexpr float HUGE_LOGIT = 1.0e30f;
-__device__ __forceinline__ bool ordinary(float m) { return m <= HUGE_LOGIT && m >= -HUGE_LOGIT; }
+// Where the reference u = m*c lies beyond 2^30 (rows masked with the type's lowest value) there is no multiply-add: u's
+// rounding would shift the terms by more than 2^64, and the product may overflow.  Two values are equal there, or at least
+// 64 binades apart.
+__device__ __forceinline__ bool ordinary(float u) { return u <= 1073741824.f && u >= -1073741824.f; }
 __device__ __forceinline__ float huge_term(float x, float m) { return m == INFINITY ? NAN : x == m ? 1.f : x == x ? 0.f : x; }
 // Keeps the compiler from widening a vector once for both this case and the ordinary one, and holding on to all of it.
 __device__ __forceinline__ uint4 opaque(uint4 r) {
@@ -250,11 +250,11 @@ __device__ __forceinline__ double rescale(float from, float to, double c) {   //
 }
 // The same for a thread's sum of terms, whose references are m*c as rounded to 32 bits; 0 from -inf, where the sum is 0.
 __device__ __forceinline__ float move_terms(float from, float to, float c) {
-    return from == to ? 1.f : ordinary(from) && ordinary(to) ? sd::ex2(from * c - to * c) : 0.f;
+    return from == to ? 1.f : ordinary(from * c) && ordinary(to * c) ? sd::ex2(from * c - to * c) : 0.f;
 }
 // The factor from sums against the rounded m*c to sums against m itself.
 __device__ __forceinline__ double unround(float m, float c) {
-    if (!ordinary(m)) return 1.0;
+    if (!ordinary(m * c)) return 1.0;
     const double x = (double)(m * c) - (double)m * (double)c, y = x * 0.69314718055994530942;
     return y * y < 1e-8 ? 1.0 + y * (1.0 + y * (0.5 + y * (1.0 / 6.0))) : exp2(x);         // the series' next term: 4e-18
 }

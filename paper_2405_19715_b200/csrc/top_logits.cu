@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                         sum *= (double)move_terms(top, wm, P.c);         // 0 so far where top is -inf
                         top = wm;
                     }
-                    if (ordinary(top) || top == -INFINITY) {
+                    if (ordinary(top * P.c) || top == -INFINITY) {
                         const float u = reference(top) * P.c;
                         const f2 neg = sd::pack2(-u, -u), c2 = sd::pack2(P.c, P.c);
                         f2 acc = sd::pack2(0.f, 0.f);

@@ -50,6 +50,8 @@ def _check_top(ctx, x, k, T):
     np.testing.assert_array_equal(tokens.cpu().numpy(), wt)
     np.testing.assert_array_equal(_np(values), wv)
     got = _np(lse)
+    # a log-sum-exp of 2^128 and more (logits near the type's end at a small T) has no f32 but infinity
+    wl = np.where(np.abs(wl) >= 2.0 ** 128, np.copysign(np.inf, wl), wl)
     bad = ~np.isfinite(wl)
     np.testing.assert_array_equal(got[bad], wl[bad])
     assert np.all(np.abs(got[~bad] - wl[~bad]) <= REL + F24 * np.abs(wl[~bad]))
@@ -106,6 +108,30 @@ def test_top_logits_hard_rows(ctx, V, dtype):
         _check_top(ctx, x, k, 1.0)
 
 
+@pytest.mark.parametrize("T", [1.0, 2.0 ** -20, 2.0 ** 20])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_logits_of_any_size(dtype, T):
+    """Offsets and scales up to the type's range, at the ends of the temperature's: nothing overflows, and what a row's logits
+    differ by is what counts."""
+    ctx = specdec.Context(1, 1)
+    V = 3000
+    base = _rows(12, 12, V, "f32").double()
+    big = float(torch.finfo(DT[dtype]).max)
+    for n, (scale, offset) in enumerate([(1, 0), (1, 1e3), (1, -1e3), (1e3, 0), (1, 1e6), (1e5, -1e8), (1e7, 0), (1, 1e9), (1e12, 0), (1e25, 1e30), (1e36, 0), (0, 1e38)]):
+        base[n] = (base[n] * scale + offset).clamp(-big, big)
+    z = base.to(DT[dtype]).contiguous()
+    values, tokens, lse = _check_top(ctx, z, 20, T)
+    assert not torch.any(torch.isnan(lse)) and torch.all(torch.isfinite(lse) | (T < 1))      # 1e38 / T is not an f32 below T = 0.3
+    w = torch.ones(12, device="cuda")
+    loss, grad = specdec.specdec_distill_step(ctx, z, values, tokens, None, w, T)
+    loss1, saved = specdec.specdec_distill(ctx, z, values, tokens, None, T)
+    grad1 = specdec.specdec_distill_backward(ctx, z, values, tokens, None, saved, w, T)
+    _check_distill(z, values, tokens, None, T, w, dtype, loss, grad)
+    _check_distill(z, values, tokens, None, T, w, dtype, loss1, grad1)
+    assert ctx.device_status() == 0
+    ctx.close()
+
+
 def test_top_logits_refusals(ctx):
     x = torch.zeros(4, 16, device="cuda")
     for args in ((x, 0), (x, 17), (torch.zeros(1, 400, device="cuda"), 257), (x, 3, 0.0), (x, 3, float("nan")), (x, 3, 1e7)):
@@ -157,9 +183,7 @@ def _check_distill(z, values, tokens, lse, T, w, dtype, loss, grad, weighted_los
         out[y] = False
         Q = q[out].sum()
         p = np.zeros(len(q))
-        norm = ln[n] if ln is not None else ro.log_sum_exp(vn[n][tn[n] >= 0], T)
-        v = vn[n][tn[n] >= 0]
-        p[y[~np.isneginf(v)]] = np.exp(v[~np.isneginf(v)] / T - norm)
+        p[y] = ro.listed_mass(vn[n][tn[n] >= 0], None if ln is None else ln[n], T)
         R = max(0.0, 1 - p.sum()) if ln is not None and Q > 0 else 0.0
         scale = abs(wn[n]) / T * (q * (p.sum() + R + (R / Q if R > 0 else 0.0)) * 2 * REL + p * 2 * F24)
         tol = scale + HALF[dtype] * (np.abs(want_g[n]) + scale) + TINY[dtype]
