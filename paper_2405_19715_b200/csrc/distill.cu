@@ -353,8 +353,12 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
         const bool plain = ordinary(u) && !zero;
         const int back = STATS ? -CHUNK : CHUNK;
         int j0 = STATS ? j_first + (own_steps - 1) * CHUNK : j_first;
+        if (STATS && !plain && !zero && own_steps > 0) {        // the slow way starts from shared memory, where another chunk may be by now
+            chunk_wait();
+            S.fetch(j0, lane, sh.chunk[warp]);
+        }
         for (int n = 0; n < own_steps; ++n, j0 += back) {
-            const bool in_registers = STATS && n == 0;
+            const bool in_registers = STATS && n == 0 && plain;
             if (!in_registers) chunk_wait();
             if (plain && straight && S.whole(j0)) {
                 if (!in_registers) {

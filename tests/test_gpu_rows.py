@@ -132,6 +132,21 @@ def test_logits_of_any_size(dtype, T):
     ctx.close()
 
 
+@pytest.mark.parametrize("V", [70000, 70003])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_logits_over_several_chunks(ctx, dtype, V):
+    """Rows whose scaled logits leave no room for a multiply-add, long enough that a warp's way back has several chunks."""
+    base = _rows(6, 6, V, "f32").double()
+    base[:4] *= torch.tensor([1e9, 1e12, 1e25, 1e36], dtype=torch.float64, device="cuda")[:, None]
+    base[4] = torch.where(torch.arange(V, device="cuda") % 7 == 3, -3e37, -3e38)
+    z = base.to(DT[dtype]).contiguous()
+    values, tokens, lse = _check_top(ctx, z, 20, 1.0)
+    w = torch.ones(6, device="cuda")
+    tokens[4] = torch.arange(20, device="cuda") * 3001 % V               # some of the largest ones, some not
+    values[4] = z[4][tokens[4].long()].float()
+    _run_all(ctx, z, values, tokens, None, w, 1.0, dtype)
+
+
 def test_top_logits_refusals(ctx):
     x = torch.zeros(4, 16, device="cuda")
     for args in ((x, 0), (x, 17), (torch.zeros(1, 400, device="cuda"), 257), (x, 3, 0.0), (x, 3, float("nan")), (x, 3, 1e7)):
