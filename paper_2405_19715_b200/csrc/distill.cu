@@ -75,8 +75,12 @@ __device__ __forceinline__ unsigned listed_bits(const uint32_t* bitmap, int j) {
     return Row<T>::N == 8 ? bytes[j] : bytes[j >> 1] >> (4 * (j & 1)) & 15u;
 }
 
-template <typename T, DistillMode MODE>
-__global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill_kernel(const __grid_constant__ DistillParams P) {
+// PER_SM: CTAs of an SM.  Four have 64 registers a thread and spill a little, which grids of several rounds more than make up
+// for: a step over 592 rows of 32000 bf16 takes 27.3 us with three and 21.0 us with four, over 2048 rows 74 us and 70 us.
+// Where three an SM hold the whole grid they are quicker: 128 rows 13.4 us against 14.8 us, their loss 9.8 us against 10.8 us.
+// A gradient alone has no such difference, and is always four.
+template <typename T, DistillMode MODE, int PER_SM>
+__global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_constant__ DistillParams P) {
     constexpr int N = Row<T>::N;
     constexpr bool STATS = MODE != DistillMode::Gradient, GRAD = MODE != DistillMode::Loss;
     extern __shared__ __align__(16) unsigned char raw[];
@@ -424,17 +428,17 @@ __global__ void __launch_bounds__(NT, MODE == DistillMode::Step ? 3 : 4) distill
     if (arrived) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <typename T, DistillMode MODE>
+template <typename T, DistillMode MODE, int PER_SM>
 cudaError_t launch_one(const DistillParams& p, int rows, size_t smem, cudaStream_t s) {
     static std::atomic<unsigned long long> allowed{0};
-    return rw::launch(distill_kernel<T, MODE>, allowed, p, rows, p.cluster, smem, s);
+    return rw::launch(distill_kernel<T, MODE, PER_SM>, allowed, p, rows, p.cluster, smem, s);
 }
 template <typename T>
-cudaError_t launch_as(const DistillParams& p, DistillMode mode, int rows, size_t smem, cudaStream_t s) {
+cudaError_t launch_as(const DistillParams& p, DistillMode mode, int rows, bool few, size_t smem, cudaStream_t s) {
     switch (mode) {
-        case DistillMode::Loss: return launch_one<T, DistillMode::Loss>(p, rows, smem, s);
-        case DistillMode::Gradient: return launch_one<T, DistillMode::Gradient>(p, rows, smem, s);
-        default: return launch_one<T, DistillMode::Step>(p, rows, smem, s);
+        case DistillMode::Loss: return few ? launch_one<T, DistillMode::Loss, 3>(p, rows, smem, s) : launch_one<T, DistillMode::Loss, 4>(p, rows, smem, s);
+        case DistillMode::Gradient: return launch_one<T, DistillMode::Gradient, 4>(p, rows, smem, s);
+        default: return few ? launch_one<T, DistillMode::Step, 3>(p, rows, smem, s) : launch_one<T, DistillMode::Step, 4>(p, rows, smem, s);
     }
 }
 
@@ -444,11 +448,11 @@ cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mod
     const int n = dtype == SPECDEC_F32 ? 4 : 8;
     const int most = (p.V + 2 * n - 2) / n;        // vectors of a row at its worst alignment
     int least = 1;
-    // a step reads its rows twice: those that are worked on at one time, three CTAs an SM, should stay in the 126 MB of L2
+    // a step reads its rows twice: those that are worked on at one time, four CTAs an SM, should stay in the 126 MB of L2
     // beside the gradient on its way out.  4096 rows of 128256 bf16: 456 us with one CTA a row, 430 us with two; 300 of them:
     // 44 us with one, 47 us with two
     if (mode == DistillMode::Step)
-        while (least < MAX_CLUSTER && std::min<long long>(rows, 3ll * sm_count / least) * most * 16 > (80ll << 20)) least *= 2;
+        while (least < MAX_CLUSTER && std::min<long long>(rows, 4ll * sm_count / least) * most * 16 > (80ll << 20)) least *= 2;
     // the bitmap of a CTA's part takes at most 128 KB of shared memory
     if (mode != DistillMode::Gradient)
         while (least < MAX_CLUSTER && most / least * n > (128 << 13)) least *= 2;
@@ -457,7 +461,8 @@ cudaError_t launch_distill(DistillParams p, specdec_dtype dtype, DistillMode mod
     const int chunks = (((most + p.cluster - 1) / p.cluster + 31) / 32 + NV - 1) / NV;
     p.slice_words = mode == DistillMode::Gradient ? 0 : chunks * NV * n;
     const size_t smem = sizeof(DistillShared) + (size_t)p.slice_words * 4 + (size_t)p.k * 20;
-    if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, smem, s);
-    if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, smem, s);
-    return launch_as<__half>(p, mode, rows, smem, s);
+    const bool few = (long long)rows * p.cluster <= 3ll * sm_count;
+    if (dtype == SPECDEC_F32) return launch_as<float>(p, mode, rows, few, smem, s);
+    if (dtype == SPECDEC_BF16) return launch_as<__nv_bfloat16>(p, mode, rows, few, smem, s);
+    return launch_as<__half>(p, mode, rows, few, smem, s);
 }
