@@ -106,15 +106,23 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
     }
     __syncthreads();
     const int left = survivors;
-    for (int i = tid; i < left; i += MERGE_THREADS) {
-        const unsigned long long key = keys[list[i]];
-        const int f = flat[list[i]];
+    // a candidate's place is counted by as many threads of a warp as there are to go round
+    int share = 1;
+    while (share < 32 && 2 * share * left <= MERGE_THREADS) share *= 2;
+    for (int i0 = 0; i0 < left; i0 += MERGE_THREADS / share) {
+        const int i = i0 + tid / share;
+        const bool on = i < left;
+        const unsigned long long key = on ? keys[list[i]] : ~0ull;
+        const int f = on ? flat[list[i]] : 0;
         int place = 0;
-        for (int q = 0; q < left; ++q) {
+#pragma unroll 4
+        for (int q = tid % share; q < left; q += share) {
             const int o = list[q];
-            place += keys[o] > key || (keys[o] == key && flat[o] < f) ? 1 : 0;
+            const unsigned long long other = keys[o];
+            place += other > key || (other == key && flat[o] < f) ? 1 : 0;
         }
-        if (place < P.M) {
+        for (int o = 1; o < share; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+        if (on && tid % share == 0 && place < P.M) {
             const size_t o = (size_t)b * P.M + place;
             P.out_scores[o] = (float)key_score(key);
             P.out_parents[o] = f / P.V;
