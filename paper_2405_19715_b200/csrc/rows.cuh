@@ -166,13 +166,17 @@ struct Slice {
         v1 = min(nvec, v0 + per);
         in0 = max(v0, shift ? 1 : 0);
         in_n = max(0, min(v1, (shift + V) / Row<T>::N) - in0);
-        chunks = ((v1 - v0 + 31) / 32 + NV - 1) / NV;
+        const int pieces = (v1 - v0 + 31) / 32;
+        chunks = (pieces + NV - 1) / NV;
+        if (SPREAD) chunks = max(chunks, min(pieces, NW));         // a short row: fewer pieces for each warp, some for all
         block = (chunks + NW - 1) / NW;
     }
     __device__ __forceinline__ int apart() const { return SPREAD ? chunks * 32 : 32; }       // vectors from one piece to the next
     // steps of a warp; where the part is spread some may have no chunk
     __device__ __forceinline__ int steps() const { return block; }
     __device__ __forceinline__ int steps_of(int warp) const { return SPREAD ? block : (chunks + NW - 1 - warp) / NW; }
+    // spread: warps that have a chunk in step 0
+    __device__ __forceinline__ int first_warps() const { return block > 0 ? (chunks + block - 1) / block : 0; }
     // first vector of a warp's chunk; v1 or more: none
     __device__ __forceinline__ int start(int step, int warp) const {
         if (!SPREAD) return v0 + (warp * (chunks / NW) + min(warp, chunks % NW) + step) * CHUNK;

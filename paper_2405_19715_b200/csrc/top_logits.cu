@@ -48,9 +48,22 @@ struct TopShared {
     uint32_t wleast[NW], wmost[NW];
     int wcount[2][NW];
     int count, n_list;                     // elements in the buffer (or that would be), length of the list
+    int want;                              // rank of the thread maximum that is the bound
     float first_bound;
     Part part, whole;                      // of the CTA, of the cluster
 };
+
+// Rank of the thread maximum that should have k of the row's elements above it.  The first chunks should hold their share of
+// the k largest, and some more: `sigmas` of its deviations and `more`.  Dealt to A threads by chance, n elements reach a share
+// 1 - exp(-n/A) of the A maxima.  The k-th maximum is reached by k in any case.
+template <typename T>
+__device__ __forceinline__ int wanted(const Slice<T, true>& S, int k, float sigmas, float more, bool by_chance) {
+    const int first = S.first_warps();
+    const float share = (float)(k * first) / (float)max(S.chunks, 1), n = share + sigmas * sqrtf(share) + more;
+    if (!by_chance) return min(k, (int)n);
+    const float A = (float)min(first * 32, S.v1 - S.v0);
+    return n < 2.f * A ? min(k, (int)(A * (1.f - expf(-n / A))) + 1) : k;
+}
 
 // The r-th largest of the 256 thread maxima, or the least of those that share the 16 leading bits of its key.  One warp;
 // r <= NT.
@@ -430,10 +443,8 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
     float top = -INFINITY;
     {
         const Slice<T, true>& S = sh.S;
-        // how many of the k largest the first chunks should hold, and some more
         const int steps = S.steps();
-        const float share = (float)P.k / (float)max(steps, 1);
-        int want = steps > 1 ? min(P.k, (int)(share + 3.5f * sqrtf(share)) + 2) : P.k;
+        if (tid == NT - 1) sh.want = wanted(S, P.k, 3.5f, 2.f, true);      // read behind a barrier
         const int real = min(S.V, S.v1 * N - S.shift) - max(0, S.v0 * N - S.shift);
         float above = -INFINITY;                    // elements must be larger than this, too; those equal to it come last
         bool strict = false;
@@ -457,7 +468,7 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                     sh.tmax[tid] = m == m ? m : -INFINITY;
                     __syncthreads();
                     if (warp == 0) {                    // while the others sum their terms
-                        const float b = rth_of_maxima(sh.tmax, want, lane);
+                        const float b = rth_of_maxima(sh.tmax, sh.want, lane);
                         if (lane == 0) sh.first_bound = b;
                     }
                 }
@@ -552,9 +563,11 @@ __global__ void __launch_bounds__(NT, PER_SM) top_logits_kernel(const __grid_con
                 break;
             }
             // too much for the lists: ties with the bound, most likely, so only what exceeds it; too little: a lower one
-            if (lost) strict = true;
-            else want = min(P.k, (int)(share + 6.f * sqrtf(share)) + 8);
-            if (tid == 0) sh.count = 0;
+            strict |= lost;
+            if (tid == 0) {
+                if (!lost) sh.want = wanted(S, P.k, 6.f, 8.f, false);
+                sh.count = 0;
+            }
             __syncthreads();
         }
     }
