@@ -22,6 +22,13 @@ __device__ __forceinline__ double key_score(unsigned long long key) {
 }
 __device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
 
+constexpr int OPEN = 0, ENDED = 1, DEAD = 2;
+struct Beam {
+    double lse;
+    float s;
+    int kind;
+};
+
 constexpr int FEW = 512;                         // candidates that are ranked as they are
 
 __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_constant__ BeamParams P) {
@@ -31,41 +38,44 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
     int* flat = reinterpret_cast<int*>(keys + n);                               // w * V + v
     __shared__ int counts[MERGE_WARPS], dead[SPECDEC_BEAM_MAX_WIDTH / 32], survivors;
     __shared__ unsigned long long bounds[8];
+    __shared__ Beam beams[SPECDEC_BEAM_MAX_WIDTH];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int w = tid; w < (P.W + 31) / 32; w += MERGE_THREADS) dead[w] = 0;
     if (tid < 8) bounds[tid] = 0;
     if (tid == 0) survivors = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the row kernel's lists
     __syncthreads();
-    for (int w = warp; w < P.W; w += MERGE_WARPS) {
+    for (int w = tid; w < P.W; w += MERGE_THREADS) {
         const int row = b * P.W + w;
-        // of an ended or empty beam parts and lists hold nothing: asked for all the same, so that nothing waits in turn
+        // of an ended or empty beam the sums hold nothing: asked for all the same, so that nothing waits in turn
         const float s = P.scores[row];
         const bool ended = P.finished && P.finished[row], live = s > -INFINITY && s < INFINITY;
         const Part part = P.parts[row];
         const double lse = (double)reference(part.m) / P.T + log(part.s);
         const bool open = live && !ended && is_finite(lse);        // a row without a finite sum offers nothing
-        if (!ended && !open && lane == 0) atomicOr(&dead[w / 32], 1 << w % 32);
-        for (int i = lane; i < P.k; i += 32) {
-            const int o = w * P.k + i;
-            const float x = P.values[(size_t)row * P.k + i];
-            const int token = P.tokens[(size_t)row * P.k + i];
-            // an empty beam's candidates all have -inf: the lowest tokens come first
-            keys[o] = ended ? (i ? 0ull : score_key(live ? (double)s : -INFINITY)) : score_key(open ? (double)s + ((double)x / P.T - lse) : -INFINITY);
-            flat[o] = w * P.V + (ended ? P.end_token : open ? token : i);
-        }
+        beams[w] = Beam{lse, live ? s : -INFINITY, ended ? ENDED : open ? OPEN : DEAD};
+        if (!ended && !open) atomicOr(&dead[w / 32], 1 << w % 32);
     }
     __syncthreads();
     int mine = 0;
-    for (int w = warp; w < P.W; w += MERGE_WARPS) {
+#pragma unroll 4
+    for (int o = tid; o < n; o += MERGE_THREADS) {
+        const int w = o / P.k, i = o - w * P.k;
+        const size_t at = (size_t)b * n + o;
+        const float x = P.values[at];
+        const int token = P.tokens[at];
+        const Beam beam = beams[w];
         // of several empty beams the first has all that can be chosen, unless its vocabulary is smaller than n_out
         bool first = true;
         for (int q = 0; q <= w / 32; ++q) first &= (dead[q] & (q < w / 32 ? ~0 : (1 << w % 32) - 1)) == 0;
-        const bool drop = (dead[w / 32] >> w % 32 & 1) && !first && P.k == P.M;
-        for (int i = lane; i < P.k; i += 32) {
-            if (drop) keys[w * P.k + i] = 0;
-            mine += keys[w * P.k + i] != 0 ? 1 : 0;
-        }
+        unsigned long long key = 0;
+        // an empty beam's candidates all have -inf: the lowest tokens come first
+        if (beam.kind == OPEN) key = score_key((double)beam.s + ((double)x / P.T - beam.lse));
+        else if (beam.kind == ENDED) key = i ? 0ull : score_key((double)beam.s);
+        else if (first || P.k < P.M) key = score_key(-INFINITY);
+        keys[o] = key;
+        flat[o] = w * P.V + (beam.kind == ENDED ? P.end_token : beam.kind == OPEN ? token : i);
+        mine += key != 0 ? 1 : 0;
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) counts[warp] = mine;
@@ -78,16 +88,23 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
         // Where h beams have r + 1 candidates at or above a value, (r + 1) h do: for r = 0, 1, 3, ... 127 the h-th largest
         // of the beams' r-th candidates, h = M / (r + 1) rounded up, is a bound
         const int r = (1 << warp) - 1, h = (P.M + r) / (r + 1);
-        if (r < P.k && h <= P.W)
-            for (int w = lane; w < P.W; w += 32) {
-                const unsigned long long key = keys[w * P.k + r];
-                int above = 0, same = 0;
-                for (int q = 0; q < P.W; ++q) {
-                    above += keys[q * P.k + r] > key ? 1 : 0;
-                    same += keys[q * P.k + r] == key ? 1 : 0;
-                }
-                if (above < h && above + same >= h) bounds[warp] = key;      // the same from every lane that gets here
+        if (r < P.k && h <= P.W) {                  // the leading 32 bits of it: a little below
+            constexpr int PER = SPECDEC_BEAM_MAX_WIDTH / 32;
+            uint32_t own[PER], prefix = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) own[i] = lane + 32 * i < P.W ? (uint32_t)(keys[(lane + 32 * i) * P.k + r] >> 32) : 0u;
+#pragma unroll 1
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t trial = prefix | (1u << bit);
+                int c = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) c += own[i] >= trial ? 1 : 0;
+                c = __reduce_add_sync(0xffffffffu, c);
+                if (c >= h) prefix = trial;
+                if (c == h) break;
             }
+            if (lane == 0) bounds[warp] = (unsigned long long)prefix << 32;
+        }
     }
     if (n > FEW) {
         __syncthreads();
