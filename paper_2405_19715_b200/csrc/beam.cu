@@ -22,7 +22,8 @@ __device__ __forceinline__ double key_score(unsigned long long key) {
 }
 __device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
 
-constexpr int OPEN = 0, ENDED = 1, DEAD = 2;
+constexpr int OPEN = 0, ENDED = 1, DEAD = 2, NOTHING = 3;
+static_assert(SPECDEC_BEAM_MAX_WIDTH <= MERGE_THREADS, "a thread for every beam");
 struct Beam {
     double lse;
     float s;
@@ -35,47 +36,60 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
     extern __shared__ __align__(16) unsigned char raw[];
     const int n = P.W * P.k;
     unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // [W][k], falling along a beam; 0: no candidate
-    int* flat = reinterpret_cast<int*>(keys + n);                               // w * V + v
-    __shared__ int counts[MERGE_WARPS], dead[SPECDEC_BEAM_MAX_WIDTH / 32], survivors;
+    int* flat = reinterpret_cast<int*>(keys + 2 * n);                           // w * V + v
+    __shared__ int counts[MERGE_WARPS], first_dead, survivors;
     __shared__ unsigned long long bounds[8];
     __shared__ Beam beams[SPECDEC_BEAM_MAX_WIDTH];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int w = tid; w < (P.W + 31) / 32; w += MERGE_THREADS) dead[w] = 0;
     if (tid < 8) bounds[tid] = 0;
-    if (tid == 0) survivors = 0;
+    if (tid == 0) {
+        survivors = 0;
+        first_dead = P.W;
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the row kernel's lists
     __syncthreads();
-    for (int w = tid; w < P.W; w += MERGE_THREADS) {
-        const int row = b * P.W + w;
+    if (tid < P.W) {
+        const int row = b * P.W + tid;
         // of an ended or empty beam the sums hold nothing: asked for all the same, so that nothing waits in turn
         const float s = P.scores[row];
         const bool ended = P.finished && P.finished[row], live = s > -INFINITY && s < INFINITY;
         const Part part = P.parts[row];
         const double lse = (double)reference(part.m) / P.T + log(part.s);
         const bool open = live && !ended && is_finite(lse);        // a row without a finite sum offers nothing
-        beams[w] = Beam{lse, live ? s : -INFINITY, ended ? ENDED : open ? OPEN : DEAD};
-        if (!ended && !open) atomicOr(&dead[w / 32], 1 << w % 32);
+        beams[tid] = Beam{lse, live ? s : -INFINITY, ended ? ENDED : open ? OPEN : DEAD};
+        if (!ended && !open) atomicMin(&first_dead, tid);
     }
     __syncthreads();
+    // of several empty beams the first has all that can be chosen, unless its vocabulary is smaller than n_out
+    if (tid < P.W && beams[tid].kind == DEAD && tid != first_dead && P.k == P.M) beams[tid].kind = NOTHING;
+    __syncthreads();
     int mine = 0;
-#pragma unroll 4
-    for (int o = tid; o < n; o += MERGE_THREADS) {
-        const int w = o / P.k, i = o - w * P.k;
-        const size_t at = (size_t)b * n + o;
-        const float x = P.values[at];
-        const int token = P.tokens[at];
-        const Beam beam = beams[w];
-        // of several empty beams the first has all that can be chosen, unless its vocabulary is smaller than n_out
-        bool first = true;
-        for (int q = 0; q <= w / 32; ++q) first &= (dead[q] & (q < w / 32 ? ~0 : (1 << w % 32) - 1)) == 0;
-        unsigned long long key = 0;
-        // an empty beam's candidates all have -inf: the lowest tokens come first
-        if (beam.kind == OPEN) key = score_key((double)beam.s + ((double)x / P.T - beam.lse));
-        else if (beam.kind == ENDED) key = i ? 0ull : score_key((double)beam.s);
-        else if (first || P.k < P.M) key = score_key(-INFINITY);
-        keys[o] = key;
-        flat[o] = w * P.V + (beam.kind == ENDED ? P.end_token : beam.kind == OPEN ? token : i);
-        mine += key != 0 ? 1 : 0;
+    const double inv_t = 1.0 / P.T;
+    constexpr int AHEAD = 4;                        // loads of a thread on their way at a time
+    for (int o0 = tid; o0 < n; o0 += AHEAD * MERGE_THREADS) {
+        float x[AHEAD];
+        int token[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int o = o0 + a * MERGE_THREADS;
+            x[a] = o < n ? P.values[(size_t)b * n + o] : 0.f;
+            token[a] = o < n ? P.tokens[(size_t)b * n + o] : 0;
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int o = o0 + a * MERGE_THREADS;
+            if (o >= n) break;
+            const int w = o / P.k, i = o - w * P.k;
+            const Beam beam = beams[w];
+            unsigned long long key = 0;
+            // an empty beam's candidates all have -inf: the lowest tokens come first
+            if (beam.kind == OPEN) key = score_key((double)beam.s + ((double)x[a] * inv_t - beam.lse));
+            else if (beam.kind == ENDED) key = i ? 0ull : score_key((double)beam.s);
+            else if (beam.kind == DEAD) key = score_key(-INFINITY);
+            keys[o] = key;
+            flat[o] = w * P.V + (beam.kind == ENDED ? P.end_token : beam.kind == OPEN ? token[a] : i);
+            mine += key != 0 ? 1 : 0;
+        }
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) counts[warp] = mine;
@@ -110,16 +124,21 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
         __syncthreads();
         for (int q = 0; q < 8; ++q) bound = bounds[q] > bound ? bounds[q] : bound;
     }
-    // survivors are listed behind the arrays: a candidate's place is counted among them
-    int* list = flat + n;
+    // survivors move behind the arrays: a candidate's place is counted among them
+    unsigned long long* left_keys = reinterpret_cast<unsigned long long*>(raw) + n;
+    int* left_flat = flat + n;
     for (int i0 = 0; i0 < n; i0 += MERGE_THREADS) {
         const int i = i0 + tid;
-        const bool on = i < n && keys[i] >= bound;
+        const unsigned long long key = i < n ? keys[i] : 0ull;
+        const bool on = key >= bound;
         const unsigned who = __ballot_sync(0xffffffffu, on);
         int at = 0;
         if (lane == 0 && who) at = atomicAdd(&survivors, __popc(who));
         at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-        if (on) list[at] = i;
+        if (on) {
+            left_keys[at] = key;
+            left_flat[at] = flat[i];
+        }
     }
     __syncthreads();
     const int left = survivors;
@@ -129,14 +148,13 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
     for (int i0 = 0; i0 < left; i0 += MERGE_THREADS / share) {
         const int i = i0 + tid / share;
         const bool on = i < left;
-        const unsigned long long key = on ? keys[list[i]] : ~0ull;
-        const int f = on ? flat[list[i]] : 0;
+        const unsigned long long key = on ? left_keys[i] : ~0ull;
+        const int f = on ? left_flat[i] : 0;
         int place = 0;
 #pragma unroll 4
         for (int q = tid % share; q < left; q += share) {
-            const int o = list[q];
-            const unsigned long long other = keys[o];
-            place += other > key || (other == key && flat[o] < f) ? 1 : 0;
+            const unsigned long long other = left_keys[q];
+            place += other > key || (other == key && left_flat[q] < f) ? 1 : 0;
         }
         for (int o = 1; o < share; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
         if (on && tid % share == 0 && place < P.M) {
@@ -285,11 +303,11 @@ cudaError_t reorder_as(const ReorderParams& p, cudaStream_t s) {
 
 }  // namespace
 
-size_t beam_merge_smem(int W, int k) { return (size_t)W * k * (sizeof(unsigned long long) + 2 * sizeof(int)); }
+size_t beam_merge_smem(int W, int k) { return 2 * (size_t)W * k * (sizeof(unsigned long long) + sizeof(int)); }
 
 cudaError_t launch_beam_merge(const BeamParams& p, int B, cudaStream_t s) {
     const size_t smem = beam_merge_smem(p.W, p.k);
-    if (smem > 48 * 1024) {
+    if (smem > 40 * 1024) {                         // the kernel has some static shared memory as well, and 48 KB without asking
         const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }

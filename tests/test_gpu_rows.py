@@ -108,6 +108,21 @@ def test_top_logits_hard_rows(ctx, V, dtype):
         _check_top(ctx, x, k, 1.0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [255, 257, 1023, 4100, 8191, 12289, 16385, 17001, 20011, 33003])
+@pytest.mark.parametrize("k", [1, 33, 65, 200, 255])
+def test_top_logits_rows_of_few_chunks(ctx, k, V, dtype):
+    """Rows that do not fill the warps' chunks, and those that just do; values with many ties, a row of two values, a rising one,
+    an outlier that leaves the others in one bin."""
+    x = _rows(k + V, 6, V, dtype)
+    x[1] = (x[1].float() * 2).round().to(DT[dtype])
+    x[2] = torch.where(torch.arange(V, device="cuda") % 5 == 2, 1.5, -0.25).to(DT[dtype])
+    x[3] = (torch.arange(V, device="cuda").float() / V * 9 - 3).to(DT[dtype])
+    x[4, V // 2] = 3e4
+    x[5] = -x[5].abs() - 1
+    _check_top(ctx, x, min(k, V), 1.0)
+
+
 @pytest.mark.parametrize("T", [1.0, 2.0 ** -20, 2.0 ** 20])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_logits_of_any_size(dtype, T):
@@ -399,6 +414,18 @@ def _beams(seed, B, W, V, dtype):
 def test_beam_select(ctx, B, W, V, M, T, dtype):
     x, scores = _beams(B + W + V, B, W, V, dtype)
     _check_beam(ctx, x, scores, M, T)
+
+
+@pytest.mark.parametrize("B,W,V,M", [(2, 32, 4000, 64), (1, 128, 1500, 64), (1, 33, 700, 248), (2, 64, 90, 90), (1, 127, 2000, 64)])
+def test_beam_select_many_candidates(ctx, B, W, V, M):
+    """Up to 8192 candidates, at the sizes where their shared memory passes what a kernel has without asking, and the bounds'
+    tables have odd ends."""
+    x, scores = _beams(B + W + V, B, W, V, "bf16")
+    scores[0, W // 2] = -float("inf")
+    _check_beam(ctx, x, scores, M, 1.0)
+    fin = (torch.arange(W, device="cuda") % 3 == 1).int().expand(B, W).contiguous()
+    _check_beam(ctx, x, scores, M, 1.0, fin, end=V - 1)
+    _check_beam(ctx, x, torch.full_like(scores, -float("inf")), M, 1.0)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
