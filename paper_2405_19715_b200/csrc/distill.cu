@@ -20,6 +20,12 @@
 // twice over, so that the way back reads no memory: one read and one write of the row.  Sums meet through distributed
 // shared memory, one record a warp.  A listed token belongs to the CTA that has its logit, which adds its part to the
 // sums and corrects its gradient.
+//
+// What it costs, on logits that are not in L2, for 4096 rows of 128256 bf16 with lists of 64: loss 170 to 186 us (5.6 to 6.2
+// TB/s), gradient 355 to 360 us (5.8 TB/s), and the step 407 to 443 us where the two take 530 us and a read and a write of the
+// logits at the rate of a copy 321 us.  Loss and gradient are within 10 % of what DRAM gives.  The step has twice the
+// exponentials (special-function unit 59 % busy, issue slots 52 %), and of the way back a sixth misses L2.  2048 rows of 32000: loss
+// 39 us, gradient 45 us, step 70 us, of which a row's waits on the meeting of its warps are the larger part.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -27,7 +33,6 @@
 namespace {
 
 using namespace rw;
-
 
 // What a warp adds to the row's sums.
 struct Record {
