@@ -462,13 +462,13 @@ int specdec_distill_step(specdec_ctx* ctx, const specdec_distill_rows* rows, con
  *   candidate (w, v) has the score  scores[b,w] + logits[b,w,v]/T - log sum_u exp(logits[b,w,u]/T)
  *   logits      dev [B, W, V]  at batch_stride and beam_stride (elements)
  *   scores      dev [B, W] f32 sum of log-probabilities so far
- *   finished    dev [B, W] int32 or NULL: a beam with a value other than 0 offers the one candidate end_token, with the
- *               score that it has; its logits are not read
- *   out_scores  dev out [B, n_out] f32    descending; equal scores in the order of (beam, token)
+ *   finished    dev [B, W] int32 or NULL: a beam with a value other than 0 offers end_token with the score that it has,
+ *               and its other tokens with the score -inf; its logits are not read
+ *   out_scores  dev out [B, n_out] f32    descending; equal scores, -inf among them, in the order of (beam, token)
  *   out_parents dev out [B, n_out] int32  beam that is continued
  *   out_tokens  dev out [B, n_out] int32  token that continues it
  * A beam whose score is not finite (an empty place), or whose row has no finite log-sum-exp (all -inf, NaN, +inf),
- * offers its tokens with the score -inf.  Where there are fewer candidates than n_out the last places hold -inf, -1, -1.
+ * offers its tokens with the score -inf: what is chosen of those is an empty place of the next step.
  * Candidates are ranked in 64 bits; out_scores is rounded once.
  *   workspace   dev, 16-byte aligned, at least specdec_beam_workspace(B, W, V, n_out) bytes; its contents do not
  *               matter before the call or after it.  Calls that overlap on the GPU need a workspace each.

@@ -83,30 +83,32 @@ def distill(z, values, tokens, lse, T, weight):
 
 
 def beam_scores(logits, scores, T, finished=None, end_token=0):
-    """[W, V] candidate scores of one entry; -inf where there is a candidate without probability, NaN where there is none."""
+    """[W, V] candidate scores of one entry."""
     W, V = logits.shape
-    out = np.empty((W, V))
+    out = np.full((W, V), -np.inf)
     for w in range(W):
         s = float(scores[w])
+        if not np.isfinite(s):
+            continue
         if finished is not None and finished[w]:
-            out[w] = np.nan
-            out[w, end_token] = s if np.isfinite(s) else -np.inf
+            out[w, end_token] = s
             continue
         lse = log_sum_exp(logits[w], T)
-        out[w] = s + np.asarray(logits[w], np.float64) / T - lse if np.isfinite(s) and np.isfinite(lse) else -np.inf
+        if np.isfinite(lse):
+            out[w] = s + np.asarray(logits[w], np.float64) / T - lse
     return out
 
 
 def beam_select(logits, scores, n_out, T, finished=None, end_token=0):
-    """(scores, parents, tokens), each [B, n_out]; the places beyond the last candidate hold -inf, -1, -1."""
-    B, W, V = logits.shape
-    s, p, t = np.full((B, n_out), -np.inf), np.full((B, n_out), -1, np.int32), np.full((B, n_out), -1, np.int32)
-    for b in range(B):
+    """(scores, parents, tokens), each [B, n_out]; equal scores, -inf among them, in the order of (beam, token)."""
+    V = logits.shape[2]
+    s, at = [], []
+    for b in range(len(logits)):
         c = beam_scores(logits[b], scores[b], T, None if finished is None else finished[b], end_token).ravel()
-        at = np.flatnonzero(~np.isnan(c))
-        at = at[np.argsort(-c[at], kind="stable")][:n_out]
-        s[b, :len(at)], p[b, :len(at)], t[b, :len(at)] = c[at], at // V, at % V
-    return s, p, t
+        at.append(np.argsort(-c, kind="stable")[:n_out])
+        s.append(c[at[-1]])
+    at = np.array(at, np.int32)
+    return np.array(s), at // V, at % V
 
 
 def beam_reorder(state, parents, lens=None):

@@ -14,7 +14,7 @@ namespace {
 
 using namespace rw;
 
-constexpr int MERGE_THREADS = 512, MERGE_WARPS = MERGE_THREADS / 32;
+constexpr int MERGE_THREADS = 512;
 
 __device__ __forceinline__ unsigned long long score_key(double s) {
     const unsigned long long b = (unsigned long long)__double_as_longlong(s + 0.0);
@@ -25,12 +25,12 @@ __device__ __forceinline__ double key_score(unsigned long long key) {
 }
 __device__ __forceinline__ bool is_finite(double x) { return x > -INFINITY && x < INFINITY; }
 
-constexpr int OPEN = 0, ENDED = 1, DEAD = 2, NOTHING = 3;
+constexpr int OPEN = 0, ENDED = 1, EMPTY = 2;
 static_assert(SPECDEC_BEAM_MAX_WIDTH <= MERGE_THREADS, "a thread for every beam");
 struct Beam {
     double lse;
     float s;
-    int kind;
+    int kind, offers;                               // how many candidates
 };
 
 constexpr int FEW = 512;                         // candidates that are ranked as they are
@@ -40,14 +40,14 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
     const int n = P.W * P.k;
     unsigned long long* keys = reinterpret_cast<unsigned long long*>(raw);      // [W][k], falling along a beam; 0: no candidate
     int* flat = reinterpret_cast<int*>(keys + 2 * n);                           // w * V + v
-    __shared__ int counts[MERGE_WARPS], first_dead, survivors;
+    __shared__ int first_idle, survivors;
     __shared__ unsigned long long bounds[8];
     __shared__ Beam beams[SPECDEC_BEAM_MAX_WIDTH];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < 8) bounds[tid] = 0;
     if (tid == 0) {
         survivors = 0;
-        first_dead = P.W;
+        first_idle = P.W;
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the row kernel's lists
     __syncthreads();
@@ -59,14 +59,14 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
         const Part part = P.parts[row];
         const double lse = (double)reference(part.m) / P.T + log(part.s);
         const bool open = live && !ended && is_finite(lse);        // a row without a finite sum offers nothing
-        beams[tid] = Beam{lse, live ? s : -INFINITY, ended ? ENDED : open ? OPEN : DEAD};
-        if (!ended && !open) atomicMin(&first_dead, tid);
+        beams[tid] = Beam{lse, s, open ? OPEN : ended && live ? ENDED : EMPTY, P.k};
+        if (!open) atomicMin(&first_idle, tid);
     }
     __syncthreads();
-    // of several empty beams the first has all that can be chosen, unless its vocabulary is smaller than n_out
-    if (tid < P.W && beams[tid].kind == DEAD && tid != first_dead && P.k == P.M) beams[tid].kind = NOTHING;
+    // the first beam that is not continued has M candidates of its own before any other beam's that score -inf, unless its
+    // vocabulary is smaller than that: of the others only what they end with can be chosen
+    if (tid < P.W && beams[tid].kind != OPEN && tid != first_idle && P.k == P.M) beams[tid].offers = beams[tid].kind == ENDED ? 1 : 0;
     __syncthreads();
-    int mine = 0;
     const double inv_t = 1.0 / P.T;
     constexpr int AHEAD = 4;                        // loads of a thread on their way at a time
     for (int o0 = tid; o0 < n; o0 += AHEAD * MERGE_THREADS) {
@@ -84,21 +84,13 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
             if (o >= n) break;
             const int w = o / P.k, i = o - w * P.k;
             const Beam beam = beams[w];
-            unsigned long long key = 0;
-            // an empty beam's candidates all have -inf: the lowest tokens come first
-            if (beam.kind == OPEN) key = score_key((double)beam.s + ((double)x[a] * inv_t - beam.lse));
-            else if (beam.kind == ENDED) key = i ? 0ull : score_key((double)beam.s);
-            else if (beam.kind == DEAD) key = score_key(-INFINITY);
-            keys[o] = key;
-            flat[o] = w * P.V + (beam.kind == ENDED ? P.end_token : beam.kind == OPEN ? token[a] : i);
-            mine += key != 0 ? 1 : 0;
+            // what scores -inf comes in the order of the tokens; an ended beam has its end token before that
+            const double score = beam.kind == OPEN ? (double)beam.s + ((double)x[a] * inv_t - beam.lse) : beam.kind == ENDED && i == 0 ? (double)beam.s : -INFINITY;
+            keys[o] = i < beam.offers ? score_key(score) : 0ull;
+            flat[o] = w * P.V + (beam.kind == OPEN ? token[a] : beam.kind == EMPTY ? i : i == 0 ? P.end_token : i <= P.end_token ? i - 1 : i);
         }
     }
-    mine = __reduce_add_sync(0xffffffffu, mine);
-    if (lane == 0) counts[warp] = mine;
     __syncthreads();
-    int total = 0;
-    for (int w = 0; w < MERGE_WARPS; ++w) total += counts[w];
 
     unsigned long long bound = 1;                   // of the candidates that can be among the M best
     if (n > FEW && warp < 8) {
@@ -166,12 +158,6 @@ __global__ void __launch_bounds__(MERGE_THREADS) beam_merge_kernel(const __grid_
             P.out_parents[o] = f / P.V;
             P.out_tokens[o] = f % P.V;
         }
-    }
-    for (int i = total + tid; i < P.M; i += MERGE_THREADS) {       // fewer candidates than places
-        const size_t o = (size_t)b * P.M + i;
-        P.out_scores[o] = -INFINITY;
-        P.out_parents[o] = -1;
-        P.out_tokens[o] = -1;
     }
 }
 

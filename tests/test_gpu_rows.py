@@ -454,6 +454,26 @@ def test_beam_select_hard_beams(ctx, V, dtype):
         _check_beam(ctx, x, scores, M, 1.0, fin, end=V - 1)
 
 
+@pytest.mark.parametrize("V", [6, 1000, 16784])
+@pytest.mark.parametrize("W", [1, 2, 5, 40])
+def test_beam_select_with_few_live_beams(ctx, W, V):
+    """Fewer finite scores than places: the rest are the lowest (beam, token) of those that score -inf, whichever kind of beam
+    they belong to."""
+    rng = np.random.default_rng(W * V)
+    B = 24
+    x, scores = _beams(W + V, B, W, V, "bf16")
+    scores[torch.from_numpy(rng.random((B, W)) < 0.4).cuda()] = float("-inf")
+    fin = torch.from_numpy((rng.random((B, W)) < 0.5).astype(np.int32)).cuda()
+    x[3:9, ::2, 1:] = float("-inf")
+    for M in (1, min(2 * W, 200), min(W * V, 200)):
+        for end in (0, 3, V - 1):
+            s, p, t = _check_beam(ctx, x, scores, M, 1.25, fin, end)
+            ws, wp, wt = ro.beam_select(_np(x), _np(scores), M, 1.25, fin.cpu().numpy(), end)
+            low = np.isneginf(ws)
+            np.testing.assert_array_equal(p[low], wp[low])
+            np.testing.assert_array_equal(t[low], wt[low])
+
+
 def test_beam_select_strides(ctx):
     B, W, V = 3, 4, 1003
     buf = torch.full((W + 1, B, V + 5), float("nan"), dtype=torch.bfloat16, device="cuda")

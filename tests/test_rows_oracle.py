@@ -71,7 +71,9 @@ def test_beam_select_against_enumeration():
     fin = np.zeros((B, W), np.int32)
     fin[1] = 1
     sc, p, t = ro.beam_select(x, s, W * V, T, fin, 2)
-    assert p[1].tolist()[W:] == [-1] * (W * V - W) and set(t[1, :W].tolist()) == {2}
+    assert set(t[1, :W].tolist()) == {2} and sorted(p[1, :W].tolist()) == list(range(W))
+    # what an ended beam does not end with has no probability, and comes in the order of (beam, token)
+    assert list(zip(p[1].tolist(), t[1].tolist()))[W:] == [(w, v) for w in range(W) for v in range(V) if v != 2] and np.all(np.isneginf(sc[1, W:]))
     assert t[0, -V:].tolist() == list(range(V)) and np.all(p[0, -V:] == 1) and np.all(np.isneginf(sc[0, -V:]))
 
 
