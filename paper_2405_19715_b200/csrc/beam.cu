@@ -5,8 +5,8 @@
 // lists and the sums behind lse_w in one pass over the logits, and one CTA per batch entry ranks the W*M candidates.
 // They are ranked in 64 bits: beams differ by sums of many terms, and two candidates that fp32 cannot tell apart would
 // come out in an order of chance.
-// The row kernel bounds it: 128 x 8 beams of 128256 bf16, 16 best, take 71 us (3.7 TB/s of logits), of which ranking is 6 us;
-// one entry of 4 beams of 32000 takes 17 us, 12 of them in the row kernel.  The ranking kernel is launched while the row kernel
+// The row kernel bounds it: 128 x 8 beams of 128256 bf16, 16 best, take 70 us (3.8 TB/s of logits), of which ranking is 4 us;
+// one entry of 4 beams of 32000 takes 16 us, 12 of them in the row kernel; 128 beams with 64 candidates each 39 us, 22 of them.  The ranking kernel is launched while the row kernel
 // runs, and waits for it on the GPU.
 #include "rows.cuh"
 

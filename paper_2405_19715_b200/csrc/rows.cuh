@@ -282,11 +282,12 @@ __device__ __forceinline__ unsigned long long cl_ld_u64(const unsigned long long
 __device__ __forceinline__ float warp_max(float v) { return sd::warp_max(v); }
 
 // CTAs per row beyond `least`: with few rows more of them share a row, while they are no more than `most` in all and have
-// 4000 vectors (64 KB) each.  Below that their meeting costs more than it saves: 5 rows of 32000 bf16 (4000 vectors) take
-// 10.6 us with one CTA each and 12.6 us with eight, 16 rows of 128256 18.9 us with one and 13.8 us with four.
+// 2000 vectors (32 KB) each.  Below that their meeting costs what it saves: the top 50 of 5 rows of 32000 bf16 (4000 vectors)
+// take 12.7 us with one CTA a row, 10.8 us with two and 12.8 us with four, of one row of 128256 11.0 us with eight as with four
+// (14.8 us), a step over 64 rows of 65536 12.6 us with one and 10.8 us with two.
 inline int cluster_size(long long rows, int nvec, int most, int least) {
     int C = least;
-    while (2 * C <= MAX_CLUSTER && rows * C * 2 <= most && nvec >= 4000 * 2 * C) C *= 2;
+    while (2 * C <= MAX_CLUSTER && rows * C * 2 <= most && nvec >= 2000 * 2 * C) C *= 2;
     return C;
 }
 
