@@ -491,20 +491,24 @@ def _arg(ctx: Context, t: torch.Tensor | None, shape: tuple, dtype) -> int | Non
     return _here(ctx, t).data_ptr()
 
 
+def _out(ctx: Context, t, like: torch.Tensor, stream, shape: tuple, dtype):
+    """(tensor, pointer) of a result: the caller's, or a new one."""
+    if t is not None:
+        return t, _arg(ctx, t, shape, dtype)
+    t = _empty(like, stream, shape, dtype)
+    return t, t.data_ptr()
+
+
 def specdec_top_logits(ctx: Context, logits, top_k: int, temperature: float = 1.0, values=None, tokens=None, lse=None,
                        stream=None):
     """specdec_top_logits of the C ABI: logits [rows, V] -> (values [rows, k] f32, tokens [rows, k] int32, lse [rows] f32)."""
     ptr, stride, rows, V = _rows_of(ctx, logits)
     k = int(top_k)
-    if values is None:
-        values = _empty(logits, stream, (rows, k), torch.float32)
-    if tokens is None:
-        tokens = _empty(logits, stream, (rows, k), torch.int32)
-    if lse is None:
-        lse = _empty(logits, stream, (rows,), torch.float32)
-    ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, temperature,
-                                          _arg(ctx, values, (rows, k), torch.float32), _arg(ctx, tokens, (rows, k), torch.int32),
-                                          _arg(ctx, lse, (rows,), torch.float32), _row_stream(ctx, stream)))
+    values, values_ptr = _out(ctx, values, logits, stream, (rows, k), torch.float32)
+    tokens, tokens_ptr = _out(ctx, tokens, logits, stream, (rows, k), torch.int32)
+    lse, lse_ptr = _out(ctx, lse, logits, stream, (rows,), torch.float32)
+    ctx._check(ctx.lib.specdec_top_logits(ctx.handle, ptr, _row_dtype(logits), stride, rows, V, k, temperature, values_ptr, tokens_ptr,
+                                          lse_ptr, _row_stream(ctx, stream)))
     return values, tokens, lse
 
 
@@ -535,12 +539,9 @@ def specdec_distill(ctx: Context, logits, values, tokens, lse, temperature: floa
     [rows], or None to renormalise over the list) -> (loss [rows] f32, saved for specdec_distill_backward)."""
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
     n = r.rows
-    if loss is None:
-        loss = _empty(logits, stream, (n,), torch.float32)
-    if saved is None:
-        saved = _empty(logits, stream, (n, DISTILL_SAVED), torch.float32)
-    ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), _arg(ctx, loss, (n,), torch.float32),
-                                       _arg(ctx, saved, (n, DISTILL_SAVED), torch.float32), _row_stream(ctx, stream)))
+    loss, loss_ptr = _out(ctx, loss, logits, stream, (n,), torch.float32)
+    saved, saved_ptr = _out(ctx, saved, logits, stream, (n, DISTILL_SAVED), torch.float32)
+    ctx._check(ctx.lib.specdec_distill(ctx.handle, C.byref(r), loss_ptr, saved_ptr, _row_stream(ctx, stream)))
     return loss, saved
 
 
@@ -562,11 +563,10 @@ def specdec_distill_step(ctx: Context, logits, values, tokens, lse, row_weight, 
     gradient of the logits' type and row stride; `grad` may be `logits` itself."""
     r = _distill_rows(ctx, logits, values, tokens, lse, temperature)
     n = r.rows
-    if loss is None:
-        loss = _empty(logits, stream, (n,), torch.float32)
+    loss, loss_ptr = _out(ctx, loss, logits, stream, (n,), torch.float32)
     grad, gptr, gstride = _gradient(ctx, stream, logits, grad)
-    ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _arg(ctx, row_weight, (n,), torch.float32),
-                                            _arg(ctx, loss, (n,), torch.float32), gptr, gstride, _row_stream(ctx, stream)))
+    ctx._check(ctx.lib.specdec_distill_step(ctx.handle, C.byref(r), _arg(ctx, row_weight, (n,), torch.float32), loss_ptr, gptr, gstride,
+                                            _row_stream(ctx, stream)))
     return loss, grad
 
 
@@ -581,19 +581,15 @@ def specdec_beam_select(ctx: Context, logits, scores, n_out: int, temperature: f
     M = int(n_out)
     beam_stride = logits.stride(1) if W > 1 else V
     batch_stride = logits.stride(0) if B > 1 else V
-    if out_scores is None:
-        out_scores = _empty(logits, stream, (B, M), torch.float32)
-    if parents is None:
-        parents = _empty(logits, stream, (B, M), torch.int32)
-    if tokens is None:
-        tokens = _empty(logits, stream, (B, M), torch.int32)
+    out_scores, scores_ptr = _out(ctx, out_scores, logits, stream, (B, M), torch.float32)
+    parents, parents_ptr = _out(ctx, parents, logits, stream, (B, M), torch.int32)
+    tokens, tokens_ptr = _out(ctx, tokens, logits, stream, (B, M), torch.int32)
     if workspace is None:
         workspace = _empty(logits, stream, ctx.lib.specdec_beam_workspace(B, W, V, M), torch.uint8)
     ctx._check(ctx.lib.specdec_beam_select(
         ctx.handle, logits.data_ptr(), _row_dtype(logits), batch_stride, beam_stride, _arg(ctx, scores, (B, W), torch.float32),
         _arg(ctx, finished, (B, W), torch.int32), end_token, temperature, B, W, V, M,
-        _arg(ctx, out_scores, (B, M), torch.float32), _arg(ctx, parents, (B, M), torch.int32), _arg(ctx, tokens, (B, M), torch.int32),
-        _arg(ctx, workspace, workspace.shape, torch.uint8), workspace.numel(), _row_stream(ctx, stream)))
+        scores_ptr, parents_ptr, tokens_ptr, _arg(ctx, workspace, workspace.shape, torch.uint8), workspace.numel(), _row_stream(ctx, stream)))
     return out_scores, parents, tokens
 
 
