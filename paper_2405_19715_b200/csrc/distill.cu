@@ -298,7 +298,9 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
             p = P.lse ? e : e > 0.0 ? 1.0 : e;      // sum p; NaN stays NaN
             R = P.lse && out > 0.f ? fmax(0.0, 1.0 - p) : 0.0;       // a draft with nothing outside the list has no rest
             mass = p + R;
-            const double out_factor = mass - (R > 0.0 ? R * (double)(s / out) : 0.0);
+            // 1/Q as 1 + in/out: with little in the list the differences here and in the loss are of numbers close to 1, and
+            // in/out, small then, is rounded on its own (a loss of 0.001 is off by 1e-9 instead of 4e-8)
+            const double out_factor = mass - (R > 0.0 ? R + R * (double)(in / out) : 0.0);
             zero = flags != 2 || s == 0.f;          // a bad list, an empty one, or no logit above -inf
             inv_s = 1.f / s;
             if (lane == 0) {
@@ -326,8 +328,8 @@ __global__ void __launch_bounds__(NT, PER_SM) distill_kernel(const __grid_consta
                 else {
                     // sum p (log p - (z - m)/T) + p log(sum exp((z - m)/T)); renormalised, p = e / sum e
                     double l = P.lse ? h : p == 0.0 ? 0.0 : h / sh.e - log(sh.e);
-                    if (p > 0.0) l += p * log((double)s * unround(m, P.c));
-                    if (R > 0.0) l += R * log(R * (double)s / (double)out);
+                    if (p > 0.0) l += p * log(((double)out + (double)in) * unround(m, P.c));
+                    if (R > 0.0) l += R * log(R + R * (double)(in / out));
                     loss = s == s ? (float)l : NAN;
                 }
                 P.loss[row_id] = loss;
